@@ -295,6 +295,90 @@ psa_status psa_dense_attention(const psa_kv_desc *desc, const void *q, float *ou
                                void *workspace, size_t workspace_bytes, void *stream);
 
 /*
+ * Attention with a sliding window and a few first tokens that stay visible ("sinks"): a static selection beside the
+ * dynamic ones above (Sec. 1, 2.2).  The query stands at position c - 1, c = ctx_lens[r], and attends token t < c if
+ * t < num_sinks or t >= c - window: softmax(q k / sqrt(d)) v over exactly these, each counted once.
+ *   window, num_sinks  >= 0, in tokens, of any size: a window of INT32_MAX attends everything, a window of 0 the sinks
+ *                      alone, both 0 nothing
+ *   out  [batch][num_q_heads][head_dim] float32; lse [batch][num_q_heads] float32 natural-log sum of exponentiated scaled
+ *        logits, may be NULL.  Where nothing is visible out = 0 and lse = -inf; a NaN in a visible key or value shows in the
+ *        outputs of its heads
+ *   workspace  psa_window_workspace_bytes of the same descriptor, window and num_sinks; holds the sticky error word
+ * Pages without a visible token are not looked at, nor are their block-table entries: they may have been freed.  What a
+ * page holds beside the visible tokens does not matter (NaN included).
+ * Shapes as for psa_dense_attention, max_blocks_per_seq up to 2^27 - 1; q 16-byte aligned.  With a second tier slices are read
+ * from where the pools are.
+ */
+size_t psa_window_workspace_bytes(const psa_kv_desc *desc, int32_t window, int32_t num_sinks);
+psa_status psa_window_attention(const psa_kv_desc *desc, const void *q, int32_t window, int32_t num_sinks, float *out, float *lse,
+                                void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * The paged cache in 4 bits: 2176 bytes where the 16-bit cache has 8192.  An element is e2m1 (a sign and one of 0, 0.5, 1,
+ * 1.5, 2, 3, 4, 6); 32 channels of a token share a power of two, stored as the byte e + 127: the smallest e >= -126 with
+ * max|x| <= 7 * 2^e.  Elements are x / 2^e to the nearest, ties to even, 6 at most.  A block of 32 with an infinity or a NaN has
+ * the byte 255 and reads as NaN.  The packed pool is [num_pages][num_kv_heads] records of PSA_PACKED_RECORD_BYTES, 16-byte aligned:
+ *      0  keys' elements [token][channel / 2], the even channel in the low half of the byte
+ *   1024  values' elements [token / 4][channel / 8][token % 4][channel % 8 / 2]
+ *   2048  keys' exponents [token][channel / 32]
+ *   2112  values' exponents [channel / 32][token]
+ * It has the tables of a 16-bit cache (block_table, ctx_lens); the pools of the descriptor are used by psa_pack_pages and
+ * psa_unpack_pages only and may be NULL elsewhere.  A descriptor with a second tier is PSA_ERR_UNSUPPORTED.
+ *
+ * psa_pack_pages: pages of the 16-bit cache to records.  page_fill, page_list, num_listed as for psa_build_block_metadata;
+ *   tokens beyond a page's fill are written as zeros and not looked at.
+ * psa_unpack_pages: records to pages of the 16-bit cache (WRITES desc->k_pool and desc->v_pool), rounded to desc->dtype: exact in
+ *   bfloat16.  page_list, num_listed as above.
+ * psa_append_kv_packed: as psa_append_kv, with the token going to the packed pool, bit for bit as psa_pack_pages packs
+ *   it (no metadata is kept); k_new and v_new [batch][num_kv_heads][head_dim] of desc->dtype, 16-byte aligned.
+ * psa_packed_attention: as psa_window_attention over the packed cache; q of desc->dtype; the dense form is a window of INT32_MAX.
+ *   Elements are used as the values they stand for, with nothing rounded but the result's binary32 sums.
+ */
+#define PSA_PACKED_RECORD_BYTES 2176
+psa_status psa_pack_pages(const psa_kv_desc *desc, void *packed_pool, const int32_t *page_fill, const int32_t *page_list,
+                          int32_t num_listed, void *stream);
+psa_status psa_unpack_pages(const psa_kv_desc *desc, const void *packed_pool, const int32_t *page_list, int32_t num_listed,
+                            void *stream);
+psa_status psa_append_kv_packed(const psa_kv_desc *desc, void *packed_pool, const void *k_new, const void *v_new,
+                                int32_t *status, void *stream);
+size_t psa_packed_workspace_bytes(const psa_kv_desc *desc, int32_t window, int32_t num_sinks);
+psa_status psa_packed_attention(const psa_kv_desc *desc, const void *packed_pool, const void *q, int32_t window,
+                                int32_t num_sinks, float *out, float *lse, void *workspace, size_t workspace_bytes,
+                                void *stream);
+
+/*
+ * Queries and keys made ready for the cache: RMS norm of every head and rotation by position, in one pass.
+ *   y = x / sqrt(mean(x^2) + eps) * w     with desc->normalize, w = the weights or 1; y = x without
+ *   pair i < rot_dim / 2 of y:  (a, b) -> (a cos u - b sin u, a sin u + b cos u),  u = position * inv_freq[i]
+ * The pair is (y[i], y[i + rot_dim / 2]), or (y[2 i], y[2 i + 1]) with desc->interleaved; channels from rot_dim on are not
+ * rotated.  Computed in binary32 (the angle in binary64) and rounded once.
+ *   q_in, k_in    [num_tokens][heads][head_dim] of desc->dtype, q_in_stride and k_in_stride elements from token to token (so
+ *                 both may lie in one projection's output); q_out, k_out likewise.  An output may be its own input, with the
+ *                 same stride; otherwise buffers do not overlap.
+ *   q_weight, k_weight  [head_dim] of desc->dtype, or NULL for ones; not looked at without desc->normalize
+ *   positions     [num_tokens] int32 (for the next token of each request: its ctx_lens before the append)
+ *   inv_freq      [rot_dim / 2] float32; may be NULL with rot_dim 0
+ * Either head count may be 0 (then its pointers may be NULL).  All but positions and inv_freq 16-byte aligned, strides multiples
+ * of 8 and at least heads * head_dim (outputs) or of any sign and size (inputs).
+ * Errors: PSA_ERR_INVALID_ARG, PSA_ERR_UNSUPPORTED (head_dim != 128, more than 65536 heads, another dtype), PSA_ERR_LAUNCH.
+ */
+typedef struct {
+    int32_t num_tokens;
+    int32_t num_q_heads;
+    int32_t num_kv_heads;
+    int32_t head_dim;           /* must be 128                                                    */
+    int32_t rot_dim;            /* channels rotated: a multiple of 8, 0 .. 128                    */
+    int32_t interleaved;        /* 0: pairs (i, i + rot_dim / 2), 1: pairs (2 i, 2 i + 1)         */
+    int32_t normalize;          /* 0 or 1                                                         */
+    int32_t dtype;              /* psa_dtype                                                      */
+    int64_t q_in_stride, k_in_stride, q_out_stride, k_out_stride;   /* elements                   */
+    float eps;                  /* finite, >= 0                                                   */
+} psa_rotate_desc;
+psa_status psa_norm_rotate(const psa_rotate_desc *desc, const void *q_in, const void *k_in, void *q_out, void *k_out,
+                           const void *q_weight, const void *k_weight, const int32_t *positions, const float *inv_freq,
+                           void *stream);
+
+/*
  * Two-tier block store (Sec. 3.1, 3.4).  All of it runs on the GPU, on `stream`; the host is not in the loop.
  *
  * psa_tier_state_bytes: bytes of psa_tier.state for these sizes (0 if they are out of range).

@@ -46,6 +46,13 @@ class _Tuning(C.Structure):
                 ("phase_events", C.c_void_p)]
 
 
+class _RotateDesc(C.Structure):
+    _fields_ = [("num_tokens", C.c_int32), ("num_q_heads", C.c_int32), ("num_kv_heads", C.c_int32),
+                ("head_dim", C.c_int32), ("rot_dim", C.c_int32), ("interleaved", C.c_int32), ("normalize", C.c_int32),
+                ("dtype", C.c_int32), ("q_in_stride", C.c_int64), ("k_in_stride", C.c_int64),
+                ("q_out_stride", C.c_int64), ("k_out_stride", C.c_int64), ("eps", C.c_float)]
+
+
 @dataclass
 class Tuning:
     chunk_blocks: int = 0
@@ -111,6 +118,22 @@ def load_library() -> C.CDLL:
         lib.psa_tier_update_workspace_bytes.argtypes = [C.POINTER(_KvDesc)]
         lib.psa_tier_update.restype = C.c_int
         lib.psa_tier_update.argtypes = [C.POINTER(_KvDesc), vp, vp, C.c_int64, C.c_int64, vp, vp, sz, vp]
+        lib.psa_window_workspace_bytes.restype = sz
+        lib.psa_window_workspace_bytes.argtypes = [C.POINTER(_KvDesc), i32, i32]
+        lib.psa_window_attention.restype = C.c_int
+        lib.psa_window_attention.argtypes = [C.POINTER(_KvDesc), vp, i32, i32, vp, vp, vp, sz, vp]
+        lib.psa_pack_pages.restype = C.c_int
+        lib.psa_pack_pages.argtypes = [C.POINTER(_KvDesc), vp, vp, vp, i32, vp]
+        lib.psa_unpack_pages.restype = C.c_int
+        lib.psa_unpack_pages.argtypes = [C.POINTER(_KvDesc), vp, vp, i32, vp]
+        lib.psa_append_kv_packed.restype = C.c_int
+        lib.psa_append_kv_packed.argtypes = [C.POINTER(_KvDesc), vp, vp, vp, vp, vp]
+        lib.psa_packed_workspace_bytes.restype = sz
+        lib.psa_packed_workspace_bytes.argtypes = [C.POINTER(_KvDesc), i32, i32]
+        lib.psa_packed_attention.restype = C.c_int
+        lib.psa_packed_attention.argtypes = [C.POINTER(_KvDesc), vp, vp, i32, i32, vp, vp, vp, sz, vp]
+        lib.psa_norm_rotate.restype = C.c_int
+        lib.psa_norm_rotate.argtypes = [C.POINTER(_RotateDesc), vp, vp, vp, vp, vp, vp, vp, vp, vp]
         lib.psa_read_device_error.restype = C.c_int
         lib.psa_read_device_error.argtypes = [vp, C.POINTER(C.c_int32), vp]
         _lib = lib
@@ -391,6 +414,215 @@ def dense_attention(kv: KvCache, q: torch.Tensor, *, workspace: torch.Tensor | N
     _check(st, "psa_dense_attention")
     out._workspace = workspace
     return out, lse
+
+
+# ---- window and sinks, the 4-bit cache, norm and rotation --------------------------------------------------------------
+PACKED_RECORD_BYTES = 2176
+EVERYTHING = 2 ** 31 - 1      # a window that holds every token
+
+
+class _On:
+    """The device a call's tensors are on, made the current one for the call, and the stream it goes to: the caller's, or that
+    device's current one."""
+
+    def __init__(self, tensor: torch.Tensor, stream):
+        if not tensor.is_cuda:
+            raise ValueError("tensors are on the GPU")
+        self.device, self.stream = tensor.device, stream
+        self.guard = None
+
+    def __enter__(self) -> int:
+        if torch.cuda.current_device() != self.device.index:
+            self.guard = torch.cuda.device(self.device)
+            self.guard.__enter__()
+        if self.stream is None:
+            return torch.cuda.current_stream().cuda_stream
+        if self.stream.device != self.device:
+            raise ValueError(f"the stream is of {self.stream.device}, the tensors are on {self.device}")
+        return self.stream.cuda_stream
+
+    def __exit__(self, *exc) -> None:
+        if self.guard is not None:
+            self.guard.__exit__(*exc)
+
+
+def _tensor(name: str, t: torch.Tensor, shape, dtype, device) -> int:
+    """The address of a contiguous tensor of just this shape, type and device."""
+    if t.shape != torch.Size(shape) or t.dtype != dtype or t.device != device or not t.is_contiguous():
+        raise ValueError(f"{name}: a contiguous {dtype} tensor of shape {tuple(shape)} on {device} is wanted, not {t.dtype} "
+                         f"{tuple(t.shape)} on {t.device} with strides {t.stride()}")
+    return t.data_ptr()
+
+
+def _scratch(nbytes: int, workspace, device, stream) -> torch.Tensor:
+    """The caller's workspace, or a new one (which is not given back to the allocator before `stream` is done with it)."""
+    if workspace is None:
+        workspace = torch.empty(nbytes, dtype=torch.uint8, device=device)
+        if stream is not None:
+            workspace.record_stream(stream)
+    elif workspace.device != device or not workspace.is_contiguous():
+        raise ValueError("workspace: a contiguous tensor on the device of q is wanted")
+    return workspace
+
+
+def _results(q: torch.Tensor, out, lse, stream):
+    made = []
+    if out is None:
+        out = torch.empty(q.shape, dtype=torch.float32, device=q.device)
+        made.append(out)
+    if lse is None:
+        lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device)
+        made.append(lse)
+    if stream is not None:
+        for t in made:
+            t.record_stream(stream)
+    return out, lse
+
+
+def window_workspace_bytes(kv: KvCache, window: int, num_sinks: int = 0) -> int:
+    d = kv.desc()
+    return int(load_library().psa_window_workspace_bytes(C.byref(d), int(window), int(num_sinks)))
+
+
+def window_attention(kv: KvCache, q: torch.Tensor, window: int, num_sinks: int = 0, *, workspace: torch.Tensor | None = None,
+                     out: torch.Tensor | None = None, lse: torch.Tensor | None = None, stream=None):
+    """psa_window_attention; returns (out float32 [B][Hq][128], lse float32 [B][Hq])."""
+    d = kv.desc()
+    lib = load_library()
+    with _On(q, stream) as handle:
+        shape, dev = (d.batch, d.num_q_heads, 128), q.device
+        _tensor("q", q, shape, kv.k_pool.dtype, dev)
+        workspace = _scratch(0 if workspace is not None else int(lib.psa_window_workspace_bytes(C.byref(d), int(window), int(num_sinks))),
+                             workspace, dev, stream)
+        out, lse = _results(q, out, lse, stream)
+        st = lib.psa_window_attention(C.byref(d), _ptr(q), int(window), int(num_sinks), _tensor("out", out, shape, torch.float32, dev),
+                                      _tensor("lse", lse, shape[:2], torch.float32, dev), _ptr(workspace), workspace.numel() * workspace.element_size(), handle)
+    _check(st, "psa_window_attention")
+    out._workspace = workspace
+    return out, lse
+
+
+class PackedCache:
+    """One layer's paged cache in 4 bits and its tables: pool uint8 [P][Hkv][2176], block_table int32 [B][max_blocks],
+    ctx_lens int32 [B], queries and new tokens of `dtype`.  The descriptor is made once: the tensors stay in place."""
+
+    def __init__(self, pool: torch.Tensor, block_table: torch.Tensor, ctx_lens: torch.Tensor, num_q_heads: int, dtype: torch.dtype):
+        if pool.dim() != 3 or block_table.dim() != 2:
+            raise ValueError("pool: [num_pages][num_kv_heads][2176], block_table: [batch][max_blocks]")
+        dev = pool.device
+        _tensor("pool", pool, (pool.shape[0], pool.shape[1], PACKED_RECORD_BYTES), torch.uint8, dev)
+        _tensor("block_table", block_table, block_table.shape, torch.int32, dev)
+        _tensor("ctx_lens", ctx_lens, (block_table.shape[0],), torch.int32, dev)
+        self.pool, self.block_table, self.ctx_lens = pool, block_table, ctx_lens
+        self.num_q_heads, self.num_kv_heads, self.dtype = int(num_q_heads), int(pool.shape[1]), dtype
+        self._desc = _KvDesc(block_table.shape[0], self.num_q_heads, self.num_kv_heads, 128, 16, pool.shape[0],
+                             block_table.shape[1], _dtype_code(dtype), None, None, _ptr(block_table), _ptr(ctx_lens), None)
+
+    @staticmethod
+    def empty_pool(num_pages: int, num_kv_heads: int, device="cuda") -> torch.Tensor:
+        return torch.zeros((num_pages, num_kv_heads, PACKED_RECORD_BYTES), dtype=torch.uint8, device=device)
+
+    def desc(self) -> _KvDesc:
+        return self._desc
+
+
+def _pages(name: str, kv: KvCache, packed: torch.Tensor, page_fill, page_list):
+    """The descriptor of the 16-bit side and the addresses of the packed pool and the lists."""
+    P, H = kv.k_pool.shape[:2]
+    dev = kv.k_pool.device
+    where = _tensor("packed pool", packed, (P, H, PACKED_RECORD_BYTES), torch.uint8, dev)
+    fill = None if page_fill is None else _tensor("page_fill", page_fill, (P,), torch.int32, dev)
+    listed = None if page_list is None else _tensor("page_list", page_list, (page_list.numel(),), torch.int32, dev)
+    return kv.desc(), where, fill, listed, 0 if page_list is None else page_list.numel()
+
+
+def pack_pages(kv: KvCache, packed: torch.Tensor, page_fill=None, page_list=None, stream=None) -> torch.Tensor:
+    """psa_pack_pages: pages of `kv` to records of the packed pool, in place; returns the pool."""
+    d, where, fill, listed, n = _pages("pack_pages", kv, packed, page_fill, page_list)
+    with _On(packed, stream) as handle:
+        st = load_library().psa_pack_pages(C.byref(d), where, fill, listed, n, handle)
+    _check(st, "psa_pack_pages")
+    return packed
+
+
+def unpack_pages(kv: KvCache, packed: torch.Tensor, page_list=None, stream=None) -> None:
+    """psa_unpack_pages: records of the packed pool to pages of `kv`, whose pools it writes."""
+    d, where, _, listed, n = _pages("unpack_pages", kv, packed, None, page_list)
+    with _On(packed, stream) as handle:
+        st = load_library().psa_unpack_pages(C.byref(d), where, listed, n, handle)
+    _check(st, "psa_unpack_pages")
+
+
+def append_kv_packed(cache: PackedCache, k_new: torch.Tensor, v_new: torch.Tensor, status: torch.Tensor | None = None,
+                     stream=None) -> None:
+    """psa_append_kv_packed: writes into cache.pool and cache.ctx_lens in place."""
+    d, dev = cache._desc, cache.pool.device
+    shape = (d.batch, d.num_kv_heads, 128)
+    with _On(cache.pool, stream) as handle:
+        st = load_library().psa_append_kv_packed(
+            C.byref(d), _ptr(cache.pool), _tensor("k_new", k_new, shape, cache.dtype, dev), _tensor("v_new", v_new, shape, cache.dtype, dev),
+            None if status is None else _tensor("status", status, (d.batch,), torch.int32, dev), handle)
+    _check(st, "psa_append_kv_packed")
+
+
+def packed_workspace_bytes(cache: PackedCache, window: int = EVERYTHING, num_sinks: int = 0) -> int:
+    return int(load_library().psa_packed_workspace_bytes(C.byref(cache._desc), int(window), int(num_sinks)))
+
+
+def packed_attention(cache: PackedCache, q: torch.Tensor, window: int = EVERYTHING, num_sinks: int = 0, *,
+                     workspace: torch.Tensor | None = None, out: torch.Tensor | None = None, lse: torch.Tensor | None = None,
+                     stream=None):
+    """psa_packed_attention; returns (out float32 [B][Hq][128], lse float32 [B][Hq])."""
+    d, dev = cache._desc, cache.pool.device
+    lib = load_library()
+    shape = (d.batch, d.num_q_heads, 128)
+    with _On(cache.pool, stream) as handle:
+        address = _tensor("q", q, shape, cache.dtype, dev)
+        workspace = _scratch(0 if workspace is not None else packed_workspace_bytes(cache, window, num_sinks), workspace, dev, stream)
+        out, lse = _results(q, out, lse, stream)
+        st = lib.psa_packed_attention(C.byref(d), _ptr(cache.pool), address, int(window), int(num_sinks),
+                                      _tensor("out", out, shape, torch.float32, dev), _tensor("lse", lse, shape[:2], torch.float32, dev),
+                                      _ptr(workspace), workspace.numel() * workspace.element_size(), handle)
+    _check(st, "psa_packed_attention")
+    out._workspace = workspace
+    return out, lse
+
+
+def _rows(name: str, t: torch.Tensor, tokens: int, dtype, device) -> int:
+    """A [tokens][heads][128] tensor whose tokens may lie any distance apart: that distance in elements."""
+    if t.dim() != 3 or t.shape[0] != tokens or t.shape[2] != 128 or t.dtype != dtype or t.device != device \
+            or (t.shape[1] > 1 and t.stride(1) != 128) or (t.shape[1] > 0 and t.stride(2) != 1):
+        raise ValueError(f"{name}: [{tokens}][heads][128] of {dtype} on {device} with contiguous heads is wanted, not {t.dtype} "
+                         f"{tuple(t.shape)} on {t.device} with strides {t.stride()}")
+    return t.stride(0) if tokens > 1 else 128 * t.shape[1]
+
+
+def norm_rotate(q: torch.Tensor, k: torch.Tensor, positions: torch.Tensor, inv_freq: torch.Tensor, *,
+                q_weight: torch.Tensor | None = None, k_weight: torch.Tensor | None = None, eps: float = 1e-6, normalize: bool = True,
+                interleaved: bool = False, q_out: torch.Tensor | None = None, k_out: torch.Tensor | None = None, stream=None):
+    """psa_norm_rotate on q [T][Hq][128] and k [T][Hkv][128] (views of one projection's output will do); rotates the
+    first 2 * len(inv_freq) channels; returns (q_out, k_out), which may be q and k themselves."""
+    T, dev, dtype = q.shape[0], q.device, q.dtype
+    made = []
+    if q_out is None:
+        made.append(q_out := torch.empty(q.shape, dtype=dtype, device=dev))
+    if k_out is None:
+        made.append(k_out := torch.empty(k.shape, dtype=dtype, device=dev))
+    if q_out.shape != q.shape or k_out.shape != k.shape:
+        raise ValueError("q_out and k_out have the shapes of q and k")
+    if stream is not None:
+        for t in made:
+            t.record_stream(stream)
+    d = _RotateDesc(T, q.shape[1], k.shape[1], 128, 2 * inv_freq.numel(), int(bool(interleaved)), int(bool(normalize)), _dtype_code(dtype),
+                    _rows("q", q, T, dtype, dev), _rows("k", k, T, dtype, dev), _rows("q_out", q_out, T, dtype, dev),
+                    _rows("k_out", k_out, T, dtype, dev), float(eps))
+    weights = [None if w is None or not normalize else _tensor(n, w, (128,), dtype, dev) for n, w in (("q_weight", q_weight), ("k_weight", k_weight))]
+    with _On(q, stream) as handle:
+        st = load_library().psa_norm_rotate(C.byref(d), _ptr(q), _ptr(k), _ptr(q_out), _ptr(k_out), *weights,
+                                            _tensor("positions", positions, (T,), torch.int32, dev),
+                                            _tensor("inv_freq", inv_freq, (inv_freq.numel(),), torch.float32, dev), handle)
+    _check(st, "psa_norm_rotate")
+    return q_out, k_out
 
 
 def tier_state_bytes(total_slices: int, num_slots: int) -> int:

@@ -274,6 +274,137 @@ psa_status psa_dense_attention(const psa_kv_desc *d, const void *q, float *out, 
     return e == hipSuccess ? PSA_OK : PSA_ERR_LAUNCH;
 }
 
+// ---- window and sinks, the 4-bit cache, norm and rotation ----------------------------------------------
+namespace {
+
+bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
+
+// Lengths stay below 2^31 tokens.
+psa_status check_window(const psa_kv_desc *d, int32_t window, int32_t num_sinks) {
+    if (window < 0 || num_sinks < 0) return PSA_ERR_INVALID_ARG;
+    return d->max_blocks_per_seq > INT32_MAX / psa::kPage ? PSA_ERR_UNSUPPORTED : PSA_OK;
+}
+
+// A descriptor whose cache is the packed pool: the 16-bit pools count only where `need_pools`.
+psa_status check_packed(const psa_kv_desc *d, const void *packed, bool need_tables, bool need_pools) {
+    if (!d) return PSA_ERR_INVALID_ARG;
+    psa_kv_desc c = *d;
+    if (!need_pools) c.k_pool = c.v_pool = packed;
+    const psa_status st = check_desc(&c, need_tables, true);
+    if (st != PSA_OK) return st;
+    if (d->tier) return PSA_ERR_UNSUPPORTED;
+    if ((d->num_pages > 0 && !packed) || !aligned16(packed)) return PSA_ERR_INVALID_ARG;
+    if (need_pools && (!aligned16(d->k_pool) || !aligned16(d->v_pool))) return PSA_ERR_INVALID_ARG;
+    return PSA_OK;
+}
+
+// As for the metadata: how many pages are listed.  `nothing`: there is nothing to do.
+psa_status check_list(const psa_kv_desc *d, const int32_t *page_list, int32_t num_listed, bool *nothing) {
+    if (num_listed < 0 || (num_listed > 0 && !page_list)) return PSA_ERR_INVALID_ARG;
+    if ((long long)(page_list ? num_listed : d->num_pages) * d->num_kv_heads > INT32_MAX) return PSA_ERR_UNSUPPORTED;
+    *nothing = (page_list && num_listed == 0) || d->num_pages == 0;
+    return PSA_OK;
+}
+
+}  // namespace
+
+size_t psa_window_workspace_bytes(const psa_kv_desc *d, int32_t window, int32_t num_sinks) {
+    if (check_desc(d, false, false) != PSA_OK || check_window(d, window, num_sinks) != PSA_OK) return 0;
+    return psa::window_workspace_bytes(d, window, num_sinks);
+}
+
+psa_status psa_window_attention(const psa_kv_desc *d, const void *q, int32_t window, int32_t num_sinks, float *out, float *lse,
+                                void *workspace, size_t workspace_bytes, void *stream) {
+    psa_status st = check_desc(d, true, true);
+    if (st == PSA_OK) st = check_window(d, window, num_sinks);
+    if (st != PSA_OK) return st;
+    psa_kv_desc tiered;
+    if (d->tier) {      // as the dense control: every slice from where the pools are
+        if ((st = check_tier(d, &tiered)) != PSA_OK) return st;
+        d = &tiered;
+    }
+    if (d->batch == 0) return PSA_OK;
+    if (!q || !out || !workspace || !aligned16(q)) return PSA_ERR_INVALID_ARG;
+    if (workspace_bytes < psa::window_workspace_bytes(d, window, num_sinks)) return PSA_ERR_WORKSPACE_TOO_SMALL;
+    hipError_t e = psa::launch_window(d, q, window, num_sinks, out, lse, workspace, (hipStream_t)stream);
+    return e == hipSuccess ? PSA_OK : PSA_ERR_LAUNCH;
+}
+
+psa_status psa_pack_pages(const psa_kv_desc *d, void *packed, const int32_t *page_fill, const int32_t *page_list,
+                          int32_t num_listed, void *stream) {
+    bool nothing = false;
+    psa_status st = check_packed(d, packed, false, true);
+    if (st == PSA_OK) st = check_list(d, page_list, num_listed, &nothing);
+    if (st != PSA_OK || nothing) return st;
+    hipError_t e = psa::launch_pack(d, packed, page_fill, page_list, num_listed, (hipStream_t)stream);
+    return e == hipSuccess ? PSA_OK : PSA_ERR_LAUNCH;
+}
+
+psa_status psa_unpack_pages(const psa_kv_desc *d, const void *packed, const int32_t *page_list, int32_t num_listed, void *stream) {
+    bool nothing = false;
+    psa_status st = check_packed(d, packed, false, true);
+    if (st == PSA_OK) st = check_list(d, page_list, num_listed, &nothing);
+    if (st != PSA_OK || nothing) return st;
+    hipError_t e = psa::launch_unpack(d, packed, page_list, num_listed, (hipStream_t)stream);
+    return e == hipSuccess ? PSA_OK : PSA_ERR_LAUNCH;
+}
+
+psa_status psa_append_kv_packed(const psa_kv_desc *d, void *packed, const void *k_new, const void *v_new, int32_t *status,
+                                void *stream) {
+    psa_status st = check_packed(d, packed, true, false);
+    if (st == PSA_OK) st = check_window(d, 0, 0);
+    if (st != PSA_OK) return st;
+    if (d->batch == 0) return PSA_OK;
+    if (!k_new || !v_new || !aligned16(k_new) || !aligned16(v_new)) return PSA_ERR_INVALID_ARG;
+    hipError_t e = psa::launch_append_packed(d, packed, k_new, v_new, status, (hipStream_t)stream);
+    return e == hipSuccess ? PSA_OK : PSA_ERR_LAUNCH;
+}
+
+size_t psa_packed_workspace_bytes(const psa_kv_desc *d, int32_t window, int32_t num_sinks) {
+    if (!d) return 0;
+    psa_kv_desc c = *d;
+    c.num_pages = 0;      // (the pool is not asked for here)
+    if (d->num_pages < 0 || d->tier || check_desc(&c, false, false) != PSA_OK || check_window(d, window, num_sinks) != PSA_OK) return 0;
+    return psa::packed_workspace_bytes(d, window, num_sinks);
+}
+
+psa_status psa_packed_attention(const psa_kv_desc *d, const void *packed, const void *q, int32_t window, int32_t num_sinks,
+                                float *out, float *lse, void *workspace, size_t workspace_bytes, void *stream) {
+    psa_status st = check_packed(d, packed, true, false);
+    if (st == PSA_OK) st = check_window(d, window, num_sinks);
+    if (st != PSA_OK) return st;
+    if (d->batch == 0) return PSA_OK;
+    if (!q || !out || !workspace || !aligned16(q)) return PSA_ERR_INVALID_ARG;
+    if (workspace_bytes < psa::packed_workspace_bytes(d, window, num_sinks)) return PSA_ERR_WORKSPACE_TOO_SMALL;
+    hipError_t e = psa::launch_packed(d, packed, q, window, num_sinks, out, lse, workspace, (hipStream_t)stream);
+    return e == hipSuccess ? PSA_OK : PSA_ERR_LAUNCH;
+}
+
+psa_status psa_norm_rotate(const psa_rotate_desc *d, const void *q_in, const void *k_in, void *q_out, void *k_out,
+                           const void *q_weight, const void *k_weight, const int32_t *positions, const float *inv_freq, void *stream) {
+    if (!d || d->num_tokens < 0 || d->num_q_heads < 0 || d->num_kv_heads < 0) return PSA_ERR_INVALID_ARG;
+    if (d->dtype != PSA_F16 && d->dtype != PSA_BF16) return PSA_ERR_UNSUPPORTED;
+    if (d->head_dim != psa::kHeadDim || d->num_q_heads > 65536 || d->num_kv_heads > 65536) return PSA_ERR_UNSUPPORTED;
+    if (d->rot_dim < 0 || d->rot_dim > d->head_dim || d->rot_dim % 8 != 0) return PSA_ERR_INVALID_ARG;
+    if (d->interleaved < 0 || d->interleaved > 1 || d->normalize < 0 || d->normalize > 1) return PSA_ERR_INVALID_ARG;
+    if (!(d->eps >= 0.0f) || isinf(d->eps)) return PSA_ERR_INVALID_ARG;      // also rejects NaN
+    const struct { const void *in, *out, *w; int64_t in_stride, out_stride; int32_t heads; } side[2] = {
+        {q_in, q_out, q_weight, d->q_in_stride, d->q_out_stride, d->num_q_heads},
+        {k_in, k_out, k_weight, d->k_in_stride, d->k_out_stride, d->num_kv_heads}};
+    for (const auto &x : side) {
+        if (x.heads == 0) continue;
+        if (x.in_stride % 8 != 0 || x.out_stride % 8 != 0) return PSA_ERR_INVALID_ARG;
+        if (d->num_tokens > 1 && x.out_stride < (int64_t)x.heads * d->head_dim) return PSA_ERR_INVALID_ARG;
+        if (d->num_tokens > 0 && (!x.in || !x.out)) return PSA_ERR_INVALID_ARG;
+        if (!aligned16(x.in) || !aligned16(x.out) || (d->normalize && !aligned16(x.w))) return PSA_ERR_INVALID_ARG;
+        if (x.in == x.out && d->num_tokens > 1 && x.in_stride != x.out_stride) return PSA_ERR_INVALID_ARG;
+    }
+    if (d->num_tokens == 0 || d->num_q_heads + d->num_kv_heads == 0) return PSA_OK;
+    if (d->rot_dim > 0 && (!positions || !inv_freq)) return PSA_ERR_INVALID_ARG;
+    hipError_t e = psa::launch_rotate(d, q_in, k_in, q_out, k_out, q_weight, k_weight, positions, inv_freq, (hipStream_t)stream);
+    return e == hipSuccess ? PSA_OK : PSA_ERR_LAUNCH;
+}
+
 size_t psa_tier_state_bytes(int64_t total_slices, int64_t num_slots) {
     if (total_slices < 1 || total_slices > INT32_MAX || num_slots < 1 || num_slots > PSA_TIER_MAX_SLOTS) return 0;
     return psa::tier_state_bytes(total_slices, num_slots);

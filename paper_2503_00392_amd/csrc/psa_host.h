@@ -66,6 +66,23 @@ hipError_t launch_means(const psa_kv_desc *d, void *means, const int32_t *page_f
 hipError_t launch_append(const psa_kv_desc *d, const void *k_new, const void *v_new, void *meta,
                          int32_t *status, hipStream_t st);
 
+// psa_window.hip, psa_packed.hip
+size_t window_workspace_bytes(const psa_kv_desc *d, int window, int num_sinks);
+hipError_t launch_window(const psa_kv_desc *d, const void *q, int window, int num_sinks, float *out, float *lse, void *ws,
+                         hipStream_t st);
+size_t packed_workspace_bytes(const psa_kv_desc *d, int window, int num_sinks);
+hipError_t launch_packed(const psa_kv_desc *d, const void *packed, const void *q, int window, int num_sinks, float *out, float *lse,
+                         void *ws, hipStream_t st);
+hipError_t launch_pack(const psa_kv_desc *d, void *packed, const int32_t *page_fill, const int32_t *page_list, int num_listed,
+                       hipStream_t st);
+hipError_t launch_unpack(const psa_kv_desc *d, const void *packed, const int32_t *page_list, int num_listed, hipStream_t st);
+hipError_t launch_append_packed(const psa_kv_desc *d, void *packed, const void *k_new, const void *v_new, int32_t *status,
+                                hipStream_t st);
+
+// psa_rotate.hip
+hipError_t launch_rotate(const psa_rotate_desc *d, const void *q_in, const void *k_in, void *q_out, void *k_out, const void *q_weight,
+                         const void *k_weight, const int32_t *positions, const float *inv_freq, hipStream_t st);
+
 // psa_decode.hip
 struct DecodePlan {
     int chunk_blocks;     // CB: ranked blocks per chunk (keys and values alike)

@@ -1,0 +1,159 @@
+// What the two attention kernels with a window share (psa_window.hip over the 16-bit cache, psa_packed.hip over the 4-bit
+// one): which tokens a query sees, the weights of the value product in parts, and how the waves' and the splits' running
+// sums come together.
+#pragma once
+
+#include "psa_attend.h"
+
+namespace psa {
+
+constexpr int kMaxSplits = 1024;      // splits of a request at most: their weights are an array in the merge's LDS
+constexpr int kSplitStride = 132;     // floats of one split's result for one head: M, l, error bits (head 0), pad, acc[128]
+
+// The query stands at position ctx - 1 and sees token t < ctx if t < sinks or t >= start = ctx - window.  The blocks that
+// hold a visible token are 0 .. head-1 and tail .. N-1, and only these are ever looked at: a table entry or a page between
+// them may hold anything.  They are counted through as 0 .. count-1.
+struct Visible {
+    int ctx, sinks, start, head, skip, count;
+    __device__ __forceinline__ int block(int i) const { return i < head ? i : i + skip; }
+    // (Without branches, and used in selections only: where lanes branched on it to overwrite an element of a vector, the
+    // compiler lost the overwriting for the first element.)
+    __device__ __forceinline__ bool sees(int t) const { return (t < ctx) & ((t < sinks) | (t >= start)); }
+    __device__ __forceinline__ bool sees_all(int b) const {
+        const int t = b * kPage;
+        return t + kPage <= ctx && (t + kPage <= sinks || t >= start);
+    }
+};
+__device__ __forceinline__ Visible make_visible(int ctx, int window, int num_sinks) {
+    Visible v;
+    v.ctx = ctx;
+    v.sinks = min(num_sinks, ctx);
+    v.start = max(0, ctx - window);
+    const int N = (ctx + kPage - 1) / kPage;
+    v.head = (v.sinks + kPage - 1) / kPage;
+    const int tail = window > 0 ? max(v.head, v.start / kPage) : N;
+    v.skip = tail - v.head;
+    v.count = v.head + N - tail;
+    return v;
+}
+
+// The weights of the value product, p in (0, 1], are given to the matrix cores in 16-bit parts in neighbouring rows of one
+// operand: upper and lower half in binary16 (22 bits of p), three parts in bfloat16 (all 24 bits: each is what truncation
+// leaves of the rest).  Two bfloat16 parts leave an error of about 1e-6 of the output; three cost nothing where a head has four rows,
+// and a second product of the same values where it has two (eight heads).
+template <int G>
+constexpr int kRowsPerHead = G == 8 ? 2 : 4;
+template <int DT, int G>
+constexpr int kProducts = (DT == 1 && G == 8) ? 2 : 1;
+
+// Bits (in the low half) of the part that row `part` of a head gets in product `which`.
+template <int DT, int G>
+__device__ __forceinline__ uint32_t weight_part(float p, int part, int which) {
+    if constexpr (DT == 0) {
+        return part < 2 ? half16<0>(p, part == 1) : 0u;
+    } else {
+        const float r1 = p - __uint_as_float(__float_as_uint(p) & 0xffff0000u);
+        const float r2 = r1 - __uint_as_float(__float_as_uint(r1) & 0xffff0000u);
+        float x;
+        if constexpr (G == 8) x = which == 0 ? (part == 0 ? p : r1) : (part == 0 ? r2 : 0.0f);
+        else x = part == 0 ? p : (part == 1 ? r1 : (part == 2 ? r2 : 0.0f));
+        return __float_as_uint(x) >> 16;
+    }
+}
+
+// The lane's sums, rows 4 rg .. 4 rg + 3 of channels 8 cl .. 8 cl + 7, to rows[head][channel]: the parts of a head are added.
+template <int G>
+__device__ __forceinline__ void store_parts(const f32x4_t (&acc)[8], float (*rows)[kHeadDim], int rg, int cl) {
+    constexpr int kHeads = 4 / kRowsPerHead<G>;
+#pragma unroll
+    for (int k = 0; k < kHeads; ++k) {
+        const int g = kHeads * rg + k;
+        if (g < G) {
+            f32x4_t *row = reinterpret_cast<f32x4_t *>(&rows[g][cl * 8]);
+#pragma unroll
+            for (int y = 0; y < 2; ++y) {
+                f32x4_t o;
+#pragma unroll
+                for (int t = 0; t < 4; ++t) {
+                    const f32x4_t &a = acc[4 * y + t];
+                    if constexpr (G == 8) o[t] = a[2 * k] + a[2 * k + 1];
+                    else o[t] = a[0] + (a[1] + a[2]);
+                }
+                row[y] = o;
+            }
+        }
+    }
+}
+
+// 2^(m - M) for a running maximum m and the maximum M over several.  Where nothing has been seen (or nothing but NaN or
+// -inf logits) m is -inf: the weight is 0, which keeps a NaN in the sums that it multiplies.
+__device__ __forceinline__ float join_weight(float m, float M) { return m == -INFINITY ? 0.0f : exp2_fast(m - M); }
+
+// One head's result from its joined numerator, denominator and maximum: 0 and -inf where no token was seen, NaN where a
+// logit or a value was NaN.
+__device__ __forceinline__ float joined_out(float n, float den) { return den == 0.0f ? 0.0f : n / den; }
+__device__ __forceinline__ float joined_lse(float M, float den) { return den == 0.0f ? -INFINITY : (M + log2_fast(den)) * kLn2; }
+
+// The four waves of a workgroup, joined through LDS: rows[wave][head][channel] and the waves' maxima and sums.  Either the
+// request's results (one split) or the split's record.
+template <int G>
+struct WaveSums {
+    float acc[4][G][kHeadDim];
+    float m[4][G], l[4][G];
+    int err[4];
+};
+template <int G>
+__device__ __forceinline__ void join_waves(const WaveSums<G> &w, int tid, bool direct, float *out, float *lse, float *record) {
+    if (!direct && tid == 0) record[2] = __int_as_float(w.err[0] | w.err[1] | w.err[2] | w.err[3]);
+    for (int idx = tid; idx < G * kHeadDim; idx += 256) {
+        const int g = idx / kHeadDim, ch = idx % kHeadDim;
+        const float M = fmaxf(fmaxf(w.m[0][g], w.m[1][g]), fmaxf(w.m[2][g], w.m[3][g]));
+        float den = 0.0f, num = 0.0f;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float f = join_weight(w.m[i][g], M);
+            den += w.l[i][g] * f;
+            num += w.acc[i][g][ch] * f;
+        }
+        if (direct) {
+            out[g * kHeadDim + ch] = joined_out(num, den);
+            if (lse && ch == 0) lse[g] = joined_lse(M, den);
+        } else {
+            float *r = record + g * kSplitStride;
+            r[4 + ch] = num;
+            if (ch == 0) { r[0] = M; r[1] = den; }
+        }
+    }
+}
+
+// Bits of the error word that a request's own workgroups find: one workgroup looks at every visible table entry of the call
+// and stores the word, where no launch follows that could do it.  (Each entry stands for a page that the other workgroups
+// read whole, so it is done before them.)
+__device__ __forceinline__ void check_tables(const KvView &kv, int window, int num_sinks, int32_t *header, int *shared_err) {
+    if (threadIdx.x == 0) *shared_err = 0;
+    __syncthreads();
+    int err = 0;
+    for (int r = threadIdx.x >> 6; r < kv.batch; r += blockDim.x >> 6) {
+        const int ctx = ctx_clamped_quiet(kv, r);
+        if (ctx != kv.ctx_lens[r]) err |= PSA_DEVERR_CTX_RANGE;
+        const Visible vis = make_visible(ctx, window, num_sinks);
+        const int32_t *table = kv.block_table + (size_t)r * kv.max_blocks;
+#pragma unroll 4
+        for (int i = threadIdx.x & 63; i < vis.count; i += 64)
+            if ((unsigned)table[vis.block(i)] >= (unsigned)kv.num_pages) err |= PSA_DEVERR_PAGE_RANGE;
+    }
+    if (err) atomicOr(shared_err, err);
+    __syncthreads();
+    if (threadIdx.x < 64) header[threadIdx.x] = threadIdx.x == 1 ? *shared_err : 0;
+}
+
+// How a call is cut: blocks of a request that may be visible at most, splits of a request.
+struct SplitPlan {
+    int blocks, nsplit;
+};
+SplitPlan visible_plan(const psa_kv_desc *d, int window, int num_sinks, int least_blocks);
+size_t visible_workspace_bytes(const psa_kv_desc *d, const SplitPlan &p);
+hipError_t launch_join(const KvView &kv, int G, int nsplit, const float *partial, float *out, float *lse, int32_t *header,
+                       hipStream_t st);
+
+}  // namespace psa

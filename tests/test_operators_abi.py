@@ -1,0 +1,185 @@
+"""Window and sinks, the 4-bit cache, norm and rotation at the boundary, without a GPU: what the host refuses (nothing is
+enqueued on those paths), the sizes of workspaces, the binding's own checks."""
+import ctypes as C
+import os
+import subprocess
+
+import numpy as np
+import pytest
+import torch
+
+import packed_reference as pr
+import paper_2503_00392_amd as psa
+from paper_2503_00392_amd import binding as pb
+
+HEADER = os.path.join(os.path.dirname(os.path.dirname(os.path.abspath(__file__))), "include", "psa.h")
+OK, INVALID, UNSUPPORTED, SMALL = 0, 1, 2, 3
+
+
+@pytest.fixture(scope="module")
+def lib():
+    if not os.path.exists(psa.library_path()):
+        from paper_2503_00392_amd import build
+        build.build()
+    return psa.load_library()
+
+
+def _desc(**kw):
+    base = dict(batch=2, num_q_heads=32, num_kv_heads=8, head_dim=128, page_size=16, num_pages=64, max_blocks_per_seq=32, dtype=0,
+                k_pool=0x1000, v_pool=0x2000, block_table=0x3000, ctx_lens=0x4000)
+    base.update(kw)
+    return pb._KvDesc(**base)
+
+
+BAD_SHAPES = [(dict(head_dim=64), UNSUPPORTED), (dict(page_size=32), UNSUPPORTED), (dict(dtype=2), UNSUPPORTED),
+              (dict(num_q_heads=24), UNSUPPORTED), (dict(num_q_heads=30), INVALID), (dict(batch=-1), INVALID),
+              (dict(num_kv_heads=0), INVALID), (dict(block_table=None), INVALID), (dict(ctx_lens=None), INVALID),
+              (dict(max_blocks_per_seq=0), INVALID), (dict(max_blocks_per_seq=1 << 27), UNSUPPORTED), (dict(num_pages=-1), INVALID)]
+
+
+def _window(lib, d, window=100, sinks=4, q=0x100, out=0x200, ws=0x300, ws_bytes=1 << 40):
+    return lib.psa_window_attention(C.byref(d), q, window, sinks, out, None, ws, ws_bytes, None)
+
+
+def _packed(lib, d, pool=0x1000, window=100, sinks=4, q=0x100, out=0x200, ws=0x300, ws_bytes=1 << 40):
+    return lib.psa_packed_attention(C.byref(d), pool, q, window, sinks, out, None, ws, ws_bytes, None)
+
+
+@pytest.mark.parametrize("kw,want", BAD_SHAPES)
+def test_attention_refuses_bad_descriptors(lib, kw, want):
+    assert _window(lib, _desc(**kw)) == want
+    assert _packed(lib, _desc(**kw)) == want
+    if not {"batch", "block_table", "ctx_lens", "max_blocks_per_seq"} & set(kw):
+        assert lib.psa_window_workspace_bytes(C.byref(_desc(**kw)), 100, 4) == 0
+        assert lib.psa_packed_workspace_bytes(C.byref(_desc(**kw)), 100, 4) == 0
+
+
+@pytest.mark.parametrize("call", [_window, _packed])
+def test_attention_refuses_bad_arguments(lib, call):
+    d = _desc()
+    for kw in (dict(window=-1), dict(sinks=-1), dict(q=None), dict(out=None), dict(ws=None), dict(q=0x108)):
+        assert call(lib, d, **kw) == INVALID, kw
+    assert call(lib, d, ws_bytes=255) == SMALL
+    assert call(lib, _desc(batch=0, block_table=None, ctx_lens=None), q=None, out=None, ws=None) == OK
+    assert lib.psa_window_attention(None, 1, 1, 1, 1, 1, 1, 1, None) == INVALID
+    assert lib.psa_packed_attention(None, 1, 1, 1, 1, 1, 1, 1, 1, None) == INVALID
+
+
+def test_window_needs_the_pools_and_the_packed_calls_do_not(lib):
+    assert _window(lib, _desc(k_pool=None)) == INVALID and _window(lib, _desc(v_pool=None)) == INVALID
+    none = _desc(k_pool=None, v_pool=None)
+    assert _packed(lib, none, ws_bytes=0) == SMALL                       # the pools were not missed
+    assert _packed(lib, none, pool=None) == INVALID and _packed(lib, none, pool=0x1004) == INVALID
+    assert lib.psa_packed_workspace_bytes(C.byref(none), 100, 0) > 0
+
+
+def test_workspaces_follow_what_can_be_visible(lib):
+    long = _desc(batch=1, max_blocks_per_seq=8192)
+    for size in (lib.psa_window_workspace_bytes, lib.psa_packed_workspace_bytes):
+        assert size(None, 1, 1) == 0 and size(C.byref(long), -1, 0) == 0 and size(C.byref(long), 0, -1) == 0
+        assert size(C.byref(long), 0, 0) == 256
+        everything = size(C.byref(long), psa.EVERYTHING, psa.EVERYTHING)
+        assert 256 <= size(C.byref(long), 64, 4) < size(C.byref(long), 16384, 4) <= everything < 1 << 28
+        assert size(C.byref(_desc(batch=0, max_blocks_per_seq=0, block_table=None, ctx_lens=None)), 9, 9) >= 256
+
+
+def test_page_calls_refuse(lib):
+    d = _desc()
+    for call in (lambda d, p=0x1000, lst=None, n=0: lib.psa_pack_pages(C.byref(d), p, None, lst, n, None),
+                 lambda d, p=0x1000, lst=None, n=0: lib.psa_unpack_pages(C.byref(d), p, lst, n, None)):
+        assert call(d, None) == INVALID and call(d, 0x1004) == INVALID
+        assert call(d, n=3) == INVALID and call(d, n=-1) == INVALID     # a count without a list
+        assert call(d, lst=0x20, n=0) == OK                             # an empty list: nothing to do
+        assert call(_desc(num_pages=0, k_pool=None, v_pool=None), None) == OK
+        assert call(_desc(k_pool=None)) == INVALID and call(_desc(v_pool=None)) == INVALID and call(_desc(v_pool=0x2008)) == INVALID
+        assert call(_desc(dtype=7)) == UNSUPPORTED and call(_desc(head_dim=64)) == UNSUPPORTED
+        assert call(_desc(num_pages=1 << 30)) == UNSUPPORTED            # 2^33 records in one launch
+    append = lambda d, p=0x1000, k=0x10, v=0x20: lib.psa_append_kv_packed(C.byref(d), p, k, v, None, None)   # noqa: E731
+    assert append(d, None) == INVALID and append(d, k=None) == INVALID and append(d, v=None) == INVALID and append(d, k=0x18) == INVALID
+    assert append(_desc(ctx_lens=None)) == INVALID and append(_desc(max_blocks_per_seq=1 << 27)) == UNSUPPORTED
+    assert append(_desc(batch=0), k=None, v=None) == OK
+
+
+def test_packed_calls_refuse_a_second_tier(lib):
+    tier = pb._Tier(0x1000, 0x2000, 1 << 20, 64, 0, None, 0)
+    d = _desc(tier=C.addressof(tier))
+    assert _packed(lib, d) == UNSUPPORTED and lib.psa_packed_workspace_bytes(C.byref(d), 1, 1) == 0
+    assert lib.psa_pack_pages(C.byref(d), 0x1000, None, None, 0, None) == UNSUPPORTED
+    assert lib.psa_unpack_pages(C.byref(d), 0x1000, None, 0, None) == UNSUPPORTED
+    assert lib.psa_append_kv_packed(C.byref(d), 0x1000, 0x10, 0x20, None, None) == UNSUPPORTED
+
+
+def _rotate(lib, q=0x100, k=0x200, q_out=0x300, k_out=0x400, qw=0x500, kw=0x600, pos=0x704, freq=0x804, **fields):
+    base = dict(num_tokens=3, num_q_heads=8, num_kv_heads=2, head_dim=128, rot_dim=128, interleaved=0, normalize=1, dtype=1,
+                q_in_stride=1536, k_in_stride=1536, q_out_stride=1024, k_out_stride=256, eps=1e-6)
+    base.update(fields)
+    return lib.psa_norm_rotate(C.byref(pb._RotateDesc(**base)), q, k, q_out, k_out, qw, kw, pos, freq, None)
+
+
+@pytest.mark.parametrize("kw,want", [
+    (dict(num_tokens=-1), INVALID), (dict(num_q_heads=-1), INVALID), (dict(num_kv_heads=-1), INVALID), (dict(num_q_heads=65537), UNSUPPORTED),
+    (dict(head_dim=64), UNSUPPORTED), (dict(dtype=2), UNSUPPORTED), (dict(rot_dim=-8), INVALID), (dict(rot_dim=136), INVALID),
+    (dict(rot_dim=60), INVALID), (dict(interleaved=2), INVALID), (dict(normalize=-1), INVALID), (dict(eps=-1e-9), INVALID),
+    (dict(eps=float("nan")), INVALID), (dict(eps=float("inf")), INVALID), (dict(q_in_stride=1540), INVALID), (dict(k_out_stride=260), INVALID),
+    (dict(q_out_stride=1016), INVALID), (dict(k_out_stride=0), INVALID), (dict(k_out_stride=-256), INVALID), (dict(q=None), INVALID),
+    (dict(k_out=None), INVALID), (dict(q=0x108), INVALID), (dict(k_out=0x402), INVALID), (dict(qw=0x508), INVALID), (dict(pos=None), INVALID),
+    (dict(freq=None), INVALID), (dict(q_out=0x100), INVALID)])          # (in place, with another stride)
+def test_norm_rotate_refuses(lib, kw, want):
+    assert _rotate(lib, **kw) == want
+
+
+def test_norm_rotate_with_nothing_to_do(lib):
+    assert _rotate(lib, num_tokens=0, q=None, k=None, q_out=None, k_out=None, pos=None) == OK
+    assert _rotate(lib, num_q_heads=0, num_kv_heads=0, q=None, k=None) == OK
+    assert lib.psa_norm_rotate(None, 1, 1, 1, 1, 1, 1, 1, 1, None) == INVALID
+
+
+def test_rotate_desc_has_the_layout_of_the_header(tmp_path):
+    lines = ['#include <stdio.h>', '#include <stddef.h>', f'#include "{HEADER}"', 'int main(void) {',
+             '  printf("size %zu\\n", sizeof(psa_rotate_desc)); printf("record %d\\n", PSA_PACKED_RECORD_BYTES);']
+    lines += [f'  printf("{f} %zu\\n", offsetof(psa_rotate_desc, {f}));' for f, _ in pb._RotateDesc._fields_] + ['  return 0;', '}']
+    (tmp_path / "layout.c").write_text("\n".join(lines))
+    subprocess.run(["gcc", "-std=c99", "-Wall", "-o", str(tmp_path / "layout"), str(tmp_path / "layout.c")], check=True)
+    got = dict(x.split() for x in subprocess.run([str(tmp_path / "layout")], check=True, capture_output=True, text=True).stdout.splitlines())
+    assert int(got.pop("size")) == C.sizeof(pb._RotateDesc) and int(got.pop("record")) == psa.PACKED_RECORD_BYTES == pr.RECORD
+    assert {f: int(v) for f, v in got.items()} == {f: getattr(pb._RotateDesc, f).offset for f, _ in pb._RotateDesc._fields_}
+
+
+def test_binding_refuses_before_it_calls():
+    table, lens = torch.zeros((2, 4), dtype=torch.int32), torch.zeros(2, dtype=torch.int32)
+    pool = psa.PackedCache.empty_pool(8, 2, device="cpu")
+    cache = psa.PackedCache(pool, table, lens, 8, torch.bfloat16)
+    q = torch.zeros((2, 8, 128), dtype=torch.bfloat16)
+    kv = psa.KvCache(*(torch.zeros((8, 2, 16, 128), dtype=torch.bfloat16) for _ in range(2)), table, lens, 8)
+    for call in (lambda: psa.packed_attention(cache, q), lambda: psa.window_attention(kv, q, 4), lambda: psa.pack_pages(kv, pool),
+                 lambda: psa.unpack_pages(kv, pool), lambda: psa.append_kv_packed(cache, q[:, :2], q[:, :2]),
+                 lambda: psa.norm_rotate(q, q, lens, torch.ones(64)),
+                 lambda: psa.PackedCache(pool[:, :, :2048], table, lens, 8, torch.bfloat16),
+                 lambda: psa.PackedCache(pool, table.long(), lens, 8, torch.bfloat16),
+                 lambda: psa.PackedCache(pool, table, lens[:1], 8, torch.bfloat16),
+                 lambda: psa.PackedCache(pool, table.t(), torch.zeros(4, dtype=torch.int32), 8, torch.bfloat16),
+                 lambda: psa.pack_pages(kv, pool[:4]), lambda: psa.pack_pages(kv, pool, page_list=lens.long()),
+                 lambda: psa.norm_rotate(q.transpose(1, 2), q, lens, torch.ones(64)),
+                 lambda: psa.norm_rotate(q[:, :, ::2], q, lens, torch.ones(64))):
+        with pytest.raises(ValueError):
+            call()
+    with pytest.raises(TypeError):
+        psa.PackedCache(pool, table, lens, 8, torch.float32)
+
+
+def test_the_reference_of_the_packed_cache():
+    """The numpy reference itself: ties, saturation, the choice of the power, NaN."""
+    x = np.zeros(128)
+    x[:10] = [7, 6.5, 5, 3.5, 2.5, 1.75, 1.25, 0.75, 0.25, -0.25]       # 7 <= 7 * 2^0
+    x[32:35] = [7.25, 5, 0.5]                                           # one octave up
+    x[64] = np.inf
+    codes, powers = pr.pack_row(x)
+    assert list(powers) == [127, 128, 255, 1]
+    assert list(codes[:10]) == [7, 7, 6, 6, 4, 4, 2, 2, 0, 8] and list(codes[32:35]) == [6, 4, 0]
+    rng = np.random.default_rng(0)
+    k, v = rng.standard_normal((2, 16, 128))
+    back = pr.unpack(pr.pack_record(k, v)[None])
+    for x, y in ((k, back[0][0]), (v, back[1][0])):
+        top = np.abs(x.reshape(16, 4, 32)).max(-1, keepdims=True)
+        assert (np.abs(x - y).reshape(16, 4, 32) <= top / 3.5).all()     # 2^e, and 2^e < max / 3.5
+        assert np.sqrt(np.mean((x - y) ** 2)) < 0.13
