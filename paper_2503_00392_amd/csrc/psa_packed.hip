@@ -180,13 +180,13 @@ struct PackedPage {
     uint4 k, v;
     uint32_t kp, vp;
 };
-__device__ __forceinline__ PackedPage load_packed(const uint8_t *rec, int lane) {
+__device__ __forceinline__ PackedPage load_packed(const uint8_t *rec, uint32_t lane) {
     PackedPage p;
-    const int rg = lane >> 4, cl = lane & 15;
-    p.k = ld16_stream(rec + cl * 64 + rg * 16);
-    p.v = ld16_stream(rec + kPackedV + lane * 16);
-    p.kp = rec[kPackedKExp + cl * 4 + rg];
-    p.vp = *reinterpret_cast<const uint32_t *>(rec + kPackedVExp + (cl >> 2) * 16 + rg * 4);
+    const uint32_t rg = lane >> 4, cl = lane & 15;
+    p.k = ld16_stream(rec + (cl * 64 + rg * 16));
+    p.v = ld16_stream(rec + kPackedV + lane * 16u);
+    p.kp = rec[kPackedKExp + (cl * 4 + rg)];
+    p.vp = *reinterpret_cast<const uint32_t *>(rec + kPackedVExp + ((cl >> 2) * 16 + rg * 4));
     return p;
 }
 __device__ __forceinline__ uint32_t word_of(const uint4 &v, int w) { return w == 0 ? v.x : (w == 1 ? v.y : (w == 2 ? v.z : v.w)); }
@@ -204,7 +204,8 @@ __global__ __launch_bounds__(256, 3) void packed_kernel(KvView kv, const uint8_t
                                                         float *__restrict__ lse, int32_t *header) {
     constexpr int kRows = kRowsPerHead<G>;
     __shared__ __attribute__((aligned(16))) WaveSums<G> sums;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, rg = lane >> 4, cl = lane & 15;
+    const int tid = threadIdx.x, lane = tid & 63, rg = lane >> 4, cl = lane & 15;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);     // (so that table entries and page addresses are scalars)
     int wg = blockIdx.x;
     if (nsplit == 1 && wg-- == 0) {
         check_tables(kv, window, num_sinks, header, &sums.err[0]);
@@ -218,6 +219,7 @@ __global__ __launch_bounds__(256, 3) void packed_kernel(KvView kv, const uint8_t
     const int per = (vis.count + nsplit - 1) / nsplit, b0 = split * per, b1 = min(vis.count, b0 + per);
 
     const int hd = cl / kRows, part = cl % kRows;
+    const WeightParts<1, G> parts(part);
     uint4 qb[4];                                         // B operand of the logits: channels 32 rg + 8 kk .. + 7
 #pragma unroll
     for (int kk = 0; kk < 4; ++kk) {
@@ -237,22 +239,29 @@ __global__ __launch_bounds__(256, 3) void packed_kernel(KvView kv, const uint8_t
             qb[kk] = make_uint4(w[0], w[1], w[2], w[3]);
         }
     }
-    float m = -INFINITY, l = 0.0f;                       // head hd: running maximum (whole wave), exp-sum (this row group)
+    float ref = 0.0f, limit = -INFINITY, l = 0.0f;       // head hd: see raise_reference; exp-sum of this row group
     f32x4_t acc[8];
 #pragma unroll
     for (int t = 0; t < 8; ++t) acc[t] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
 
     const int32_t *table = kv.block_table + (size_t)r * kv.max_blocks;
-    auto record_of = [&](int b) __attribute__((always_inline)) {
+    auto load_block = [&](int b) __attribute__((always_inline)) {
         const int page = table[vis.block(min(b, b1 - 1))], at = clamp_page_quiet(page, kv.num_pages);
         if (page != at) err |= PSA_DEVERR_PAGE_RANGE;
-        return kv.k_pool + ((size_t)at * kv.num_kv_heads + h) * kPackedBytes;
+        return load_packed(kv.k_pool + ((size_t)at * kv.num_kv_heads + h) * kPackedBytes, lane);
     };
+    PackedPage next[2];
+    if (b0 + 2 * wave < b1) {
+        next[0] = load_block(b0 + 2 * wave);
+        next[1] = load_block(b0 + 2 * wave + 1);
+    }
     for (int b = b0 + 2 * wave; b < b1; b += 8) {
-        PackedPage pg[2];
-#pragma unroll
-        for (int y = 0; y < 2; ++y) pg[y] = load_packed(record_of(b + y), lane);
-        float sc[8];
+        PackedPage pg[2] = {next[0], next[1]};
+        if (b + 8 < b1) {                                // the next pair is under way while this one is worked on
+            next[0] = load_block(b + 8);
+            next[1] = load_block(b + 9);
+        }
+        float sc[8];                                     // (not yet scaled)
 #pragma unroll
         for (int y = 0; y < 2; ++y) {
             f32x4_t d = {0.0f, 0.0f, 0.0f, 0.0f};
@@ -261,9 +270,8 @@ __global__ __launch_bounds__(256, 3) void packed_kernel(KvView kv, const uint8_t
             for (int kk = 0; kk < 4; ++kk) d = mfma_16x16x32<1>(from_elements<1>(word_of(pg[y].k, kk), ks), qb[kk], d);
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                float x = d[j];
-                if constexpr (DT == 0) x += dpp_f<0xB1>(x);
-                sc[4 * y + j] = x * kScaleLog2;
+                sc[4 * y + j] = d[j];
+                if constexpr (DT == 0) sc[4 * y + j] += dpp_f<0xB1>(sc[4 * y + j]);
             }
             const int lb = vis.block(b + y);
             if (b + y >= b1 || !vis.sees_all(lb)) {
@@ -278,55 +286,35 @@ __global__ __launch_bounds__(256, 3) void packed_kernel(KvView kv, const uint8_t
                 pg[y].v = make_uint4(vw[0], vw[1], vw[2], vw[3]);
             }
         }
-        float bm = fmaxf(fmaxf(fmaxf(sc[0], sc[1]), fmaxf(sc[2], sc[3])), fmaxf(fmaxf(sc[4], sc[5]), fmaxf(sc[6], sc[7])));
-        bm = fmaxf(bm, __shfl_xor(bm, 16));
-        bm = fmaxf(bm, __shfl_xor(bm, 32));
-        const float mn = fmaxf(m, bm), ref = mn == -INFINITY ? 0.0f : mn;
-        const float alpha = exp2_fast(m - ref);
+        const float bm = kScaleLog2 * fmaxf(fmaxf(fmaxf(sc[0], sc[1]), fmaxf(sc[2], sc[3])), fmaxf(fmaxf(sc[4], sc[5]), fmaxf(sc[6], sc[7])));
+        if (__ballot(bm > limit)) raise_reference(bm, ref, limit, l, acc, rg);
         float p[8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) p[j] = exp2_fast(sc[j] - ref);
-        l = l * alpha + (((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7])));
-        m = mn;
-        if (__ballot(alpha != 1.0f)) {                   // a maximum has moved: each accumulator row by its head's factor
-#pragma unroll
-            for (int x = 0; x < 4; ++x) {
-                const float a = __shfl(alpha, 4 * rg + x);
-#pragma unroll
-                for (int t = 0; t < 8; ++t) acc[t][x] *= a;
-            }
-        }
+        for (int j = 0; j < 8; ++j) p[j] = exp2_fast(fmaf(sc[j], kScaleLog2, -ref));
+        l += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
         uint4 a[kProducts<1, G>];
 #pragma unroll
-        for (int y = 0; y < kProducts<1, G>; ++y) {
-            uint32_t w[8];
-#pragma unroll
-            for (int j = 0; j < 8; ++j) w[j] = weight_part<1, G>(p[j], part, y);
-            a[y] = make_uint4(w[0] | (w[1] << 16), w[2] | (w[3] << 16), w[4] | (w[5] << 16), w[6] | (w[7] << 16));
-        }
+        for (int y = 0; y < kProducts<1, G>; ++y)
+            a[y] = make_uint4(parts(p[0], p[1], y), parts(p[2], p[3], y), parts(p[4], p[5], y), parts(p[6], p[7], y));
         uint4 vv[8];                                     // [page][token]: eight channels in bfloat16
 #pragma unroll
         for (int y = 0; y < 2; ++y)
 #pragma unroll
             for (int j = 0; j < 4; ++j)
                 vv[4 * y + j] = from_elements<1>(word_of(pg[y].v, j), power_of((pg[y].vp >> (8 * j)) & 0xffu));
-#pragma unroll
-        for (int t = 0; t < 8; ++t) {
-            uint32_t w[4];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const uint32_t x = word_of(vv[2 * j], t >> 1), y = word_of(vv[2 * j + 1], t >> 1);
-                w[j] = (t & 1) ? (x >> 16) | (y & 0xffff0000u) : (x & 0xffffu) | (y << 16);
-            }
-            const uint4 bv = make_uint4(w[0], w[1], w[2], w[3]);
+        static_for<8>([&](auto t) __attribute__((always_inline)) {
+            constexpr int w = t / 2;
+            constexpr bool odd = t & 1;
+            const uint4 bv = make_uint4(pick_halves<odd>(word_of(vv[0], w), word_of(vv[1], w)), pick_halves<odd>(word_of(vv[2], w), word_of(vv[3], w)),
+                                        pick_halves<odd>(word_of(vv[4], w), word_of(vv[5], w)), pick_halves<odd>(word_of(vv[6], w), word_of(vv[7], w)));
 #pragma unroll
             for (int y = 0; y < kProducts<1, G>; ++y) acc[t] = mfma_16x16x32<1>(a[y], bv, acc[t]);
-        }
+        });
     }
     l += __shfl_xor(l, 16);
     l += __shfl_xor(l, 32);
-    store_parts<G>(acc, sums.acc[wave], rg, cl);
-    if (rg == 0 && hd < G && part == 0) { sums.m[wave][hd] = m; sums.l[wave][hd] = l; }
+    store_parts<1, G>(acc, sums.acc[wave], rg, cl);
+    if (rg == 0 && hd < G && part == 0) { sums.m[wave][hd] = limit == -INFINITY ? -INFINITY : ref; sums.l[wave][hd] = l; }
     const bool bad_ctx = __ballot(err & PSA_DEVERR_CTX_RANGE) != 0ull, bad_page = __ballot(err & PSA_DEVERR_PAGE_RANGE) != 0ull;
     if (lane == 0) sums.err[wave] = (bad_ctx ? PSA_DEVERR_CTX_RANGE : 0) | (bad_page ? PSA_DEVERR_PAGE_RANGE : 0);
     __syncthreads();

@@ -37,7 +37,7 @@ __device__ __forceinline__ Visible make_visible(int ctx, int window, int num_sin
     return v;
 }
 
-// The weights of the value product, p in (0, 1], are given to the matrix cores in 16-bit parts in neighbouring rows of one
+// The weights of the value product, p in (0, 2^kSlack], are given to the matrix cores in 16-bit parts in neighbouring rows of one
 // operand: upper and lower half in binary16 (22 bits of p), three parts in bfloat16 (all 24 bits: each is what truncation
 // leaves of the rest).  Two bfloat16 parts leave an error of about 1e-6 of the output; three cost nothing where a head has four rows,
 // and a second product of the same values where it has two (eight heads).
@@ -46,23 +46,59 @@ constexpr int kRowsPerHead = G == 8 ? 2 : 4;
 template <int DT, int G>
 constexpr int kProducts = (DT == 1 && G == 8) ? 2 : 1;
 
-// Bits (in the low half) of the part that row `part` of a head gets in product `which`.
+// The part of two weights that the lane's row gets in product `which`, packed.  What to take off is a mask per lane, so that
+// nothing branches: bfloat16 parts are p, p less its upper 16 bits, and that less its own upper 16 bits, each cut to 16 bits
+// (a row beyond the parts gets the last part again, and store_parts leaves it out).  Binary16 parts are p cut to 11
+// bits, exactly, and the rest, rounded.
 template <int DT, int G>
-__device__ __forceinline__ uint32_t weight_part(float p, int part, int which) {
-    if constexpr (DT == 0) {
-        return part < 2 ? half16<0>(p, part == 1) : 0u;
-    } else {
-        const float r1 = p - __uint_as_float(__float_as_uint(p) & 0xffff0000u);
-        const float r2 = r1 - __uint_as_float(__float_as_uint(r1) & 0xffff0000u);
-        float x;
-        if constexpr (G == 8) x = which == 0 ? (part == 0 ? p : r1) : (part == 0 ? r2 : 0.0f);
-        else x = part == 0 ? p : (part == 1 ? r1 : (part == 2 ? r2 : 0.0f));
-        return __float_as_uint(x) >> 16;
+struct WeightParts {
+    uint32_t m1, m2;
+    __device__ __forceinline__ explicit WeightParts(int part) {
+        if constexpr (DT == 0) {
+            m1 = part == 0 ? 0xffffe000u : ~0u;
+            m2 = part == 0 ? 0u : 0xffffe000u;
+        } else if constexpr (G == 8) {
+            m1 = part == 0 ? 0u : 0xffff0000u;
+            m2 = part == 0 ? 0xffff0000u : 0u;
+        } else {
+            m1 = part == 0 ? 0u : 0xffff0000u;
+            m2 = part < 2 ? 0u : 0xffff0000u;
+        }
     }
+    __device__ __forceinline__ static float masked(float x, uint32_t m) { return __uint_as_float(__float_as_uint(x) & m); }
+    __device__ __forceinline__ float pick(float p, int which) const {
+        if constexpr (DT == 0) {
+            return masked(p, m1) - masked(p, m2);
+        } else if constexpr (G == 8) {
+            if (which == 0) return p - masked(p, m1);
+            const float r = p - masked(p, 0xffff0000u);
+            return masked(r - masked(r, 0xffff0000u), m2);
+        } else {
+            const float r = p - masked(p, m1);
+            return r - masked(r, m2);
+        }
+    }
+    __device__ __forceinline__ uint32_t operator()(float p0, float p1, int which) const {
+        const float a = pick(p0, which), b = pick(p1, which);
+        if constexpr (DT == 0) {
+            const half2_t h = {(_Float16)a, (_Float16)b};
+            return __builtin_bit_cast(uint32_t, h);
+        } else {
+            return upper_halves(a, b);
+        }
+    }
+    __device__ __forceinline__ static uint32_t upper_halves(float a, float b) {
+        return __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u);
+    }
+};
+// The lower (or upper) 16-bit halves of two words, packed.
+template <bool UPPER>
+__device__ __forceinline__ uint32_t pick_halves(uint32_t a, uint32_t b) {
+    return __builtin_amdgcn_perm(b, a, UPPER ? 0x07060302u : 0x05040100u);
 }
 
 // The lane's sums, rows 4 rg .. 4 rg + 3 of channels 8 cl .. 8 cl + 7, to rows[head][channel]: the parts of a head are added.
-template <int G>
+template <int DT, int G>
 __device__ __forceinline__ void store_parts(const f32x4_t (&acc)[8], float (*rows)[kHeadDim], int rg, int cl) {
     constexpr int kHeads = 4 / kRowsPerHead<G>;
 #pragma unroll
@@ -77,11 +113,33 @@ __device__ __forceinline__ void store_parts(const f32x4_t (&acc)[8], float (*row
                 for (int t = 0; t < 4; ++t) {
                     const f32x4_t &a = acc[4 * y + t];
                     if constexpr (G == 8) o[t] = a[2 * k] + a[2 * k + 1];
+                    else if constexpr (DT == 0) o[t] = a[0] + a[1];
                     else o[t] = a[0] + (a[1] + a[2]);
                 }
                 row[y] = o;
             }
         }
+    }
+}
+
+// Weights are taken against a reference that follows the running maximum of a head in leaps: a logit (log2 units) may exceed it
+// by kSlack before it moves, so that most steps exchange nothing between the lanes and rescale nothing; a weight is 2^kSlack
+// at most.  `limit` is ref + kSlack, -inf until the first logit above -inf (ref is 0 then).  All lanes of the wave
+// together; bm is the maximum over the lane's own tokens.
+constexpr float kSlack = 8.0f;
+__device__ __forceinline__ void raise_reference(float bm, float &ref, float &limit, float &l, f32x4_t (&acc)[8], int rg) {
+    bm = fmaxf(bm, __shfl_xor(bm, 16));
+    bm = fmaxf(bm, __shfl_xor(bm, 32));
+    const bool raise = bm > limit;
+    const float alpha = raise ? (limit == -INFINITY ? 1.0f : exp2_fast(ref - bm)) : 1.0f;      // (nothing, or NaN, in the sums before)
+    ref = raise ? bm : ref;
+    limit = raise ? bm + kSlack : limit;
+    l *= alpha;
+#pragma unroll
+    for (int x = 0; x < 4; ++x) {
+        const float a = __shfl(alpha, 4 * rg + x);
+#pragma unroll
+        for (int t = 0; t < 8; ++t) acc[t][x] *= a;
     }
 }
 

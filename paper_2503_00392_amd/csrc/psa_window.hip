@@ -19,7 +19,8 @@ __global__ __launch_bounds__(256, 3) void window_kernel(KvView kv, const uint8_t
     constexpr int kRows = kRowsPerHead<G>;
     __shared__ uint4 stage[4][16 * 17];                  // per wave: a key slice on its way into the operand's layout
     __shared__ __attribute__((aligned(16))) WaveSums<G> sums;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, rg = lane >> 4, cl = lane & 15;
+    const int tid = threadIdx.x, lane = tid & 63, rg = lane >> 4, cl = lane & 15;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);     // (so that what hangs on it is a scalar)
     int wg = blockIdx.x;
     if (nsplit == 1 && wg-- == 0) {
         check_tables(kv, window, num_sinks, header, &sums.err[0]);
@@ -33,13 +34,14 @@ __global__ __launch_bounds__(256, 3) void window_kernel(KvView kv, const uint8_t
     const int per = (vis.count + nsplit - 1) / nsplit, b0 = split * per, b1 = min(vis.count, b0 + per);
 
     const int hd = cl / kRows, part = cl % kRows;
+    const WeightParts<DT, G> parts(part);
     uint4 qb[4];                                         // B operand of the logits: a head's rows all hold its query
 #pragma unroll
     for (int kk = 0; kk < 4; ++kk) {
         qb[kk] = make_uint4(0, 0, 0, 0);
         if (hd < G) qb[kk] = ld16(q + ((size_t)(r * kv.num_q_heads + h * G + hd) * kHeadDim + (4 * kk + rg) * 8) * 2);
     }
-    float m = -INFINITY, l = 0.0f;                       // head hd: running maximum (whole wave), exp-sum (this row group)
+    float ref = 0.0f, limit = -INFINITY, l = 0.0f;       // head hd: see raise_reference; exp-sum of this row group
     f32x4_t acc[8];
 #pragma unroll
     for (int t = 0; t < 8; ++t) acc[t] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
@@ -78,44 +80,28 @@ __global__ __launch_bounds__(256, 3) void window_kernel(KvView kv, const uint8_t
                 v.r[j] = seen ? v.r[j] : make_uint4(0, 0, 0, 0);
             }
         }
-        float bm = fmaxf(fmaxf(sc[0], sc[1]), fmaxf(sc[2], sc[3]));
-        bm = fmaxf(bm, __shfl_xor(bm, 16));
-        bm = fmaxf(bm, __shfl_xor(bm, 32));
-        const float mn = fmaxf(m, bm), ref = mn == -INFINITY ? 0.0f : mn;
-        const float alpha = exp2_fast(m - ref);
+        const float bm = fmaxf(fmaxf(sc[0], sc[1]), fmaxf(sc[2], sc[3]));
+        if (__ballot(bm > limit)) raise_reference(bm, ref, limit, l, acc, rg);
         float p[4];
 #pragma unroll
         for (int j = 0; j < 4; ++j) p[j] = exp2_fast(sc[j] - ref);
-        l = l * alpha + ((p[0] + p[1]) + (p[2] + p[3]));
-        m = mn;
-        if (__ballot(alpha != 1.0f)) {                   // a maximum has moved: each accumulator row by its head's factor
+        l += (p[0] + p[1]) + (p[2] + p[3]);
+        uint2 a[kProducts<DT, G>];
 #pragma unroll
-            for (int x = 0; x < 4; ++x) {
-                const float a = __shfl(alpha, 4 * rg + x);
+        for (int y = 0; y < kProducts<DT, G>; ++y) a[y] = make_uint2(parts(p[0], p[1], y), parts(p[2], p[3], y));
+        static_for<8>([&](auto t) __attribute__((always_inline)) {
+            constexpr int w = t / 2;
+            constexpr bool odd = t & 1;
+            const uint2 bv = make_uint2(pick_halves<odd>(pick_word(v.r[0], w), pick_word(v.r[1], w)),
+                                        pick_halves<odd>(pick_word(v.r[2], w), pick_word(v.r[3], w)));
 #pragma unroll
-                for (int t = 0; t < 8; ++t) acc[t][x] *= a;
-            }
-        }
-#pragma unroll
-        for (int y = 0; y < kProducts<DT, G>; ++y) {
-            uint32_t w[4];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) w[j] = weight_part<DT, G>(p[j], part, y);
-            const uint2 a = make_uint2(w[0] | (w[1] << 16), w[2] | (w[3] << 16));
-#pragma unroll
-            for (int t = 0; t < 8; ++t) {
-                const uint32_t w0 = pick_word(v.r[0], t >> 1), w1 = pick_word(v.r[1], t >> 1);
-                const uint32_t w2 = pick_word(v.r[2], t >> 1), w3 = pick_word(v.r[3], t >> 1);
-                const uint2 bv = (t & 1) ? make_uint2((w0 >> 16) | (w1 & 0xffff0000u), (w2 >> 16) | (w3 & 0xffff0000u))
-                                         : make_uint2((w0 & 0xffffu) | (w1 << 16), (w2 & 0xffffu) | (w3 << 16));
-                acc[t] = mfma_16x16x16<DT>(a, bv, acc[t]);
-            }
-        }
+            for (int y = 0; y < kProducts<DT, G>; ++y) acc[t] = mfma_16x16x16<DT>(a[y], bv, acc[t]);
+        });
     }
     l += __shfl_xor(l, 16);
     l += __shfl_xor(l, 32);
-    store_parts<G>(acc, sums.acc[wave], rg, cl);
-    if (rg == 0 && hd < G && part == 0) { sums.m[wave][hd] = m; sums.l[wave][hd] = l; }
+    store_parts<DT, G>(acc, sums.acc[wave], rg, cl);
+    if (rg == 0 && hd < G && part == 0) { sums.m[wave][hd] = limit == -INFINITY ? -INFINITY : ref; sums.l[wave][hd] = l; }
     const bool bad_ctx = __ballot(err & PSA_DEVERR_CTX_RANGE) != 0ull, bad_page = __ballot(err & PSA_DEVERR_PAGE_RANGE) != 0ull;
     if (lane == 0) sums.err[wave] = (bad_ctx ? PSA_DEVERR_CTX_RANGE : 0) | (bad_page ? PSA_DEVERR_PAGE_RANGE : 0);
     __syncthreads();
