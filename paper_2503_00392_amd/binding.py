@@ -421,62 +421,50 @@ PACKED_RECORD_BYTES = 2176
 EVERYTHING = 2 ** 31 - 1      # a window that holds every token
 
 
-class _On:
-    """The device a call's tensors are on, made the current one for the call, and the stream it goes to: the caller's, or that
-    device's current one."""
-
-    def __init__(self, tensor: torch.Tensor, stream):
-        if not tensor.is_cuda:
-            raise ValueError("tensors are on the GPU")
-        self.device, self.stream = tensor.device, stream
-        self.guard = None
-
-    def __enter__(self) -> int:
-        if torch.cuda.current_device() != self.device.index:
-            self.guard = torch.cuda.device(self.device)
-            self.guard.__enter__()
-        if self.stream is None:
-            return torch.cuda.current_stream().cuda_stream
-        if self.stream.device != self.device:
-            raise ValueError(f"the stream is of {self.stream.device}, the tensors are on {self.device}")
-        return self.stream.cuda_stream
-
-    def __exit__(self, *exc) -> None:
-        if self.guard is not None:
-            self.guard.__exit__(*exc)
+def _device_of(t: torch.Tensor) -> int:
+    at = t.get_device()
+    if at < 0:
+        raise ValueError("tensors are on the GPU")
+    return at
 
 
-def _tensor(name: str, t: torch.Tensor, shape, dtype, device) -> int:
+def _launch(call, at: int, stream, *args) -> int:
+    """call(*args, stream) with the tensors' device as the current one, on the caller's stream or that device's current one."""
+    if stream is None:
+        handle = torch._C._cuda_getCurrentRawStream(at)
+    elif stream.device.index != at:
+        raise ValueError(f"the stream is of {stream.device}, the tensors are on cuda:{at}")
+    else:
+        handle = stream.cuda_stream
+    if torch.cuda.current_device() == at:
+        return call(*args, handle)
+    with torch.cuda.device(at):
+        return call(*args, handle)
+
+
+def _tensor(name: str, t: torch.Tensor, shape: tuple, dtype, at: int) -> int:
     """The address of a contiguous tensor of just this shape, type and device."""
-    if t.shape != torch.Size(shape) or t.dtype != dtype or t.device != device or not t.is_contiguous():
-        raise ValueError(f"{name}: a contiguous {dtype} tensor of shape {tuple(shape)} on {device} is wanted, not {t.dtype} "
+    if t.shape != shape or t.dtype is not dtype or t.get_device() != at or not t.is_contiguous():
+        raise ValueError(f"{name}: a contiguous {dtype} tensor of shape {tuple(shape)} on device {at} is wanted, not {t.dtype} "
                          f"{tuple(t.shape)} on {t.device} with strides {t.stride()}")
     return t.data_ptr()
 
 
-def _scratch(nbytes: int, workspace, device, stream) -> torch.Tensor:
-    """The caller's workspace, or a new one (which is not given back to the allocator before `stream` is done with it)."""
-    if workspace is None:
-        workspace = torch.empty(nbytes, dtype=torch.uint8, device=device)
-        if stream is not None:
-            workspace.record_stream(stream)
-    elif workspace.device != device or not workspace.is_contiguous():
-        raise ValueError("workspace: a contiguous tensor on the device of q is wanted")
-    return workspace
-
-
-def _results(q: torch.Tensor, out, lse, stream):
+def _results(q: torch.Tensor, workspace, nbytes, out, lse, at: int, stream):
+    """The caller's buffers, or new ones (not given back to the allocator before `stream` is done with them)."""
     made = []
+    if workspace is None:
+        made.append(workspace := torch.empty(nbytes(), dtype=torch.uint8, device=q.device))
+    elif workspace.get_device() != at or not workspace.is_contiguous():
+        raise ValueError("workspace: a contiguous tensor on the device of q is wanted")
     if out is None:
-        out = torch.empty(q.shape, dtype=torch.float32, device=q.device)
-        made.append(out)
+        made.append(out := torch.empty(q.shape, dtype=torch.float32, device=q.device))
     if lse is None:
-        lse = torch.empty(q.shape[:2], dtype=torch.float32, device=q.device)
-        made.append(lse)
+        made.append(lse := torch.empty(q.shape[:2], dtype=torch.float32, device=q.device))
     if stream is not None:
         for t in made:
             t.record_stream(stream)
-    return out, lse
+    return workspace, out, lse
 
 
 def window_workspace_bytes(kv: KvCache, window: int, num_sinks: int = 0) -> int:
@@ -487,17 +475,12 @@ def window_workspace_bytes(kv: KvCache, window: int, num_sinks: int = 0) -> int:
 def window_attention(kv: KvCache, q: torch.Tensor, window: int, num_sinks: int = 0, *, workspace: torch.Tensor | None = None,
                      out: torch.Tensor | None = None, lse: torch.Tensor | None = None, stream=None):
     """psa_window_attention; returns (out float32 [B][Hq][128], lse float32 [B][Hq])."""
-    d = kv.desc()
-    lib = load_library()
-    with _On(q, stream) as handle:
-        shape, dev = (d.batch, d.num_q_heads, 128), q.device
-        _tensor("q", q, shape, kv.k_pool.dtype, dev)
-        workspace = _scratch(0 if workspace is not None else int(lib.psa_window_workspace_bytes(C.byref(d), int(window), int(num_sinks))),
-                             workspace, dev, stream)
-        out, lse = _results(q, out, lse, stream)
-        st = lib.psa_window_attention(C.byref(d), _ptr(q), int(window), int(num_sinks), _tensor("out", out, shape, torch.float32, dev),
-                                      _tensor("lse", lse, shape[:2], torch.float32, dev), _ptr(workspace), workspace.numel() * workspace.element_size(), handle)
-    _check(st, "psa_window_attention")
+    d, at = kv.desc(), _device_of(q)
+    shape = (d.batch, d.num_q_heads, 128)
+    where = _tensor("q", q, shape, kv.k_pool.dtype, at)
+    workspace, out, lse = _results(q, workspace, lambda: window_workspace_bytes(kv, window, num_sinks), out, lse, at, stream)
+    _check(_launch(load_library().psa_window_attention, at, stream, d, where, window, num_sinks, _tensor("out", out, shape, torch.float32, at),
+                   _tensor("lse", lse, shape[:2], torch.float32, at), workspace.data_ptr(), workspace.nbytes), "psa_window_attention")
     out._workspace = workspace
     return out, lse
 
@@ -509,10 +492,10 @@ class PackedCache:
     def __init__(self, pool: torch.Tensor, block_table: torch.Tensor, ctx_lens: torch.Tensor, num_q_heads: int, dtype: torch.dtype):
         if pool.dim() != 3 or block_table.dim() != 2:
             raise ValueError("pool: [num_pages][num_kv_heads][2176], block_table: [batch][max_blocks]")
-        dev = pool.device
-        _tensor("pool", pool, (pool.shape[0], pool.shape[1], PACKED_RECORD_BYTES), torch.uint8, dev)
-        _tensor("block_table", block_table, block_table.shape, torch.int32, dev)
-        _tensor("ctx_lens", ctx_lens, (block_table.shape[0],), torch.int32, dev)
+        at = pool.get_device()
+        _tensor("pool", pool, (pool.shape[0], pool.shape[1], PACKED_RECORD_BYTES), torch.uint8, at)
+        _tensor("block_table", block_table, block_table.shape, torch.int32, at)
+        _tensor("ctx_lens", ctx_lens, (block_table.shape[0],), torch.int32, at)
         self.pool, self.block_table, self.ctx_lens = pool, block_table, ctx_lens
         self.num_q_heads, self.num_kv_heads, self.dtype = int(num_q_heads), int(pool.shape[1]), dtype
         self._desc = _KvDesc(block_table.shape[0], self.num_q_heads, self.num_kv_heads, 128, 16, pool.shape[0],
@@ -526,43 +509,40 @@ class PackedCache:
         return self._desc
 
 
-def _pages(name: str, kv: KvCache, packed: torch.Tensor, page_fill, page_list):
-    """The descriptor of the 16-bit side and the addresses of the packed pool and the lists."""
+def _pages(kv: KvCache, packed: torch.Tensor, page_fill, page_list):
+    """The device, the descriptor of the 16-bit side, and the addresses of the packed pool and the lists."""
     P, H = kv.k_pool.shape[:2]
-    dev = kv.k_pool.device
-    where = _tensor("packed pool", packed, (P, H, PACKED_RECORD_BYTES), torch.uint8, dev)
-    fill = None if page_fill is None else _tensor("page_fill", page_fill, (P,), torch.int32, dev)
-    listed = None if page_list is None else _tensor("page_list", page_list, (page_list.numel(),), torch.int32, dev)
-    return kv.desc(), where, fill, listed, 0 if page_list is None else page_list.numel()
+    at = _device_of(packed)
+    if kv.k_pool.get_device() != at or kv.v_pool.get_device() != at:
+        raise ValueError("both caches are on one device")
+    where = _tensor("packed pool", packed, (P, H, PACKED_RECORD_BYTES), torch.uint8, at)
+    fill = None if page_fill is None else _tensor("page_fill", page_fill, (P,), torch.int32, at)
+    n = 0 if page_list is None else page_list.numel()
+    listed = None if page_list is None else _tensor("page_list", page_list, (n,), torch.int32, at)
+    return at, kv.desc(), where, fill, listed, n
 
 
 def pack_pages(kv: KvCache, packed: torch.Tensor, page_fill=None, page_list=None, stream=None) -> torch.Tensor:
     """psa_pack_pages: pages of `kv` to records of the packed pool, in place; returns the pool."""
-    d, where, fill, listed, n = _pages("pack_pages", kv, packed, page_fill, page_list)
-    with _On(packed, stream) as handle:
-        st = load_library().psa_pack_pages(C.byref(d), where, fill, listed, n, handle)
-    _check(st, "psa_pack_pages")
+    at, d, where, fill, listed, n = _pages(kv, packed, page_fill, page_list)
+    _check(_launch(load_library().psa_pack_pages, at, stream, d, where, fill, listed, n), "psa_pack_pages")
     return packed
 
 
 def unpack_pages(kv: KvCache, packed: torch.Tensor, page_list=None, stream=None) -> None:
     """psa_unpack_pages: records of the packed pool to pages of `kv`, whose pools it writes."""
-    d, where, _, listed, n = _pages("unpack_pages", kv, packed, None, page_list)
-    with _On(packed, stream) as handle:
-        st = load_library().psa_unpack_pages(C.byref(d), where, listed, n, handle)
-    _check(st, "psa_unpack_pages")
+    at, d, where, _, listed, n = _pages(kv, packed, None, page_list)
+    _check(_launch(load_library().psa_unpack_pages, at, stream, d, where, listed, n), "psa_unpack_pages")
 
 
 def append_kv_packed(cache: PackedCache, k_new: torch.Tensor, v_new: torch.Tensor, status: torch.Tensor | None = None,
                      stream=None) -> None:
     """psa_append_kv_packed: writes into cache.pool and cache.ctx_lens in place."""
-    d, dev = cache._desc, cache.pool.device
+    d, at = cache._desc, _device_of(cache.pool)
     shape = (d.batch, d.num_kv_heads, 128)
-    with _On(cache.pool, stream) as handle:
-        st = load_library().psa_append_kv_packed(
-            C.byref(d), _ptr(cache.pool), _tensor("k_new", k_new, shape, cache.dtype, dev), _tensor("v_new", v_new, shape, cache.dtype, dev),
-            None if status is None else _tensor("status", status, (d.batch,), torch.int32, dev), handle)
-    _check(st, "psa_append_kv_packed")
+    _check(_launch(load_library().psa_append_kv_packed, at, stream, d, cache.pool.data_ptr(), _tensor("k_new", k_new, shape, cache.dtype, at),
+                   _tensor("v_new", v_new, shape, cache.dtype, at),
+                   None if status is None else _tensor("status", status, (d.batch,), torch.int32, at)), "psa_append_kv_packed")
 
 
 def packed_workspace_bytes(cache: PackedCache, window: int = EVERYTHING, num_sinks: int = 0) -> int:
@@ -573,28 +553,25 @@ def packed_attention(cache: PackedCache, q: torch.Tensor, window: int = EVERYTHI
                      workspace: torch.Tensor | None = None, out: torch.Tensor | None = None, lse: torch.Tensor | None = None,
                      stream=None):
     """psa_packed_attention; returns (out float32 [B][Hq][128], lse float32 [B][Hq])."""
-    d, dev = cache._desc, cache.pool.device
-    lib = load_library()
+    d, at = cache._desc, _device_of(cache.pool)
     shape = (d.batch, d.num_q_heads, 128)
-    with _On(cache.pool, stream) as handle:
-        address = _tensor("q", q, shape, cache.dtype, dev)
-        workspace = _scratch(0 if workspace is not None else packed_workspace_bytes(cache, window, num_sinks), workspace, dev, stream)
-        out, lse = _results(q, out, lse, stream)
-        st = lib.psa_packed_attention(C.byref(d), _ptr(cache.pool), address, int(window), int(num_sinks),
-                                      _tensor("out", out, shape, torch.float32, dev), _tensor("lse", lse, shape[:2], torch.float32, dev),
-                                      _ptr(workspace), workspace.numel() * workspace.element_size(), handle)
-    _check(st, "psa_packed_attention")
+    where = _tensor("q", q, shape, cache.dtype, at)
+    workspace, out, lse = _results(q, workspace, lambda: packed_workspace_bytes(cache, window, num_sinks), out, lse, at, stream)
+    _check(_launch(load_library().psa_packed_attention, at, stream, d, cache.pool.data_ptr(), where, window, num_sinks,
+                   _tensor("out", out, shape, torch.float32, at), _tensor("lse", lse, shape[:2], torch.float32, at),
+                   workspace.data_ptr(), workspace.nbytes), "psa_packed_attention")
     out._workspace = workspace
     return out, lse
 
 
-def _rows(name: str, t: torch.Tensor, tokens: int, dtype, device) -> int:
+def _rows(name: str, t: torch.Tensor, tokens: int, dtype, at: int) -> int:
     """A [tokens][heads][128] tensor whose tokens may lie any distance apart: that distance in elements."""
-    if t.dim() != 3 or t.shape[0] != tokens or t.shape[2] != 128 or t.dtype != dtype or t.device != device \
-            or (t.shape[1] > 1 and t.stride(1) != 128) or (t.shape[1] > 0 and t.stride(2) != 1):
-        raise ValueError(f"{name}: [{tokens}][heads][128] of {dtype} on {device} with contiguous heads is wanted, not {t.dtype} "
-                         f"{tuple(t.shape)} on {t.device} with strides {t.stride()}")
-    return t.stride(0) if tokens > 1 else 128 * t.shape[1]
+    shape, stride = t.shape, t.stride()
+    if len(shape) != 3 or shape[0] != tokens or shape[2] != 128 or t.dtype is not dtype or t.get_device() != at \
+            or (shape[1] > 1 and stride[1] != 128) or (shape[1] > 0 and stride[2] != 1):
+        raise ValueError(f"{name}: [{tokens}][heads][128] of {dtype} on device {at} with contiguous heads is wanted, not {t.dtype} "
+                         f"{tuple(shape)} on {t.device} with strides {stride}")
+    return stride[0] if tokens > 1 else 128 * shape[1]
 
 
 def norm_rotate(q: torch.Tensor, k: torch.Tensor, positions: torch.Tensor, inv_freq: torch.Tensor, *,
@@ -602,26 +579,26 @@ def norm_rotate(q: torch.Tensor, k: torch.Tensor, positions: torch.Tensor, inv_f
                 interleaved: bool = False, q_out: torch.Tensor | None = None, k_out: torch.Tensor | None = None, stream=None):
     """psa_norm_rotate on q [T][Hq][128] and k [T][Hkv][128] (views of one projection's output will do); rotates the
     first 2 * len(inv_freq) channels; returns (q_out, k_out), which may be q and k themselves."""
-    T, dev, dtype = q.shape[0], q.device, q.dtype
+    T, dtype, at = q.shape[0], q.dtype, _device_of(q)
     made = []
     if q_out is None:
-        made.append(q_out := torch.empty(q.shape, dtype=dtype, device=dev))
+        made.append(q_out := torch.empty(q.shape, dtype=dtype, device=q.device))
     if k_out is None:
-        made.append(k_out := torch.empty(k.shape, dtype=dtype, device=dev))
+        made.append(k_out := torch.empty(k.shape, dtype=dtype, device=q.device))
     if q_out.shape != q.shape or k_out.shape != k.shape:
         raise ValueError("q_out and k_out have the shapes of q and k")
     if stream is not None:
         for t in made:
             t.record_stream(stream)
-    d = _RotateDesc(T, q.shape[1], k.shape[1], 128, 2 * inv_freq.numel(), int(bool(interleaved)), int(bool(normalize)), _dtype_code(dtype),
-                    _rows("q", q, T, dtype, dev), _rows("k", k, T, dtype, dev), _rows("q_out", q_out, T, dtype, dev),
-                    _rows("k_out", k_out, T, dtype, dev), float(eps))
-    weights = [None if w is None or not normalize else _tensor(n, w, (128,), dtype, dev) for n, w in (("q_weight", q_weight), ("k_weight", k_weight))]
-    with _On(q, stream) as handle:
-        st = load_library().psa_norm_rotate(C.byref(d), _ptr(q), _ptr(k), _ptr(q_out), _ptr(k_out), *weights,
-                                            _tensor("positions", positions, (T,), torch.int32, dev),
-                                            _tensor("inv_freq", inv_freq, (inv_freq.numel(),), torch.float32, dev), handle)
-    _check(st, "psa_norm_rotate")
+    half = inv_freq.numel()
+    d = _RotateDesc(T, q.shape[1], k.shape[1], 128, 2 * half, bool(interleaved), bool(normalize), _dtype_code(dtype),
+                    _rows("q", q, T, dtype, at), _rows("k", k, T, dtype, at), _rows("q_out", q_out, T, dtype, at),
+                    _rows("k_out", k_out, T, dtype, at), eps)
+    _check(_launch(load_library().psa_norm_rotate, at, stream, d, q.data_ptr(), k.data_ptr(), q_out.data_ptr(), k_out.data_ptr(),
+                   None if q_weight is None or not normalize else _tensor("q_weight", q_weight, (128,), dtype, at),
+                   None if k_weight is None or not normalize else _tensor("k_weight", k_weight, (128,), dtype, at),
+                   _tensor("positions", positions, (T,), torch.int32, at), _tensor("inv_freq", inv_freq, (half,), torch.float32, at)),
+           "psa_norm_rotate")
     return q_out, k_out
 
 

@@ -191,32 +191,32 @@ __device__ __forceinline__ PackedPage load_packed(const uint8_t *rec, uint32_t l
 }
 __device__ __forceinline__ uint32_t word_of(const uint4 &v, int w) { return w == 0 ? v.x : (w == 1 ? v.y : (w == 2 ? v.z : v.w)); }
 
-// grid: one workgroup of four waves per split and (request, KV head); with one split a first workgroup more, which writes
-// the error word.  A wave takes pairs of visible blocks.
+// grid: one workgroup of four waves per split and (request, KV head), before them the one that checks the tables (if any).  A wave takes pairs of visible blocks.
 //   logits  D[token][row] = K[token][channel] Q[channel][row], four 16x16x32 products a block: elements and power become
 //           bfloat16, exactly.  A query in bfloat16 stands in all rows of its head; one in binary16 is split into two
 //           bfloat16 parts in neighbouring rows (8 + 3 bits, exact), whose sums are added.
 //   values  D[row][channel] += P[row][token] V[token][channel], one 16x16x32 product for eight channels of the pair's 32
 //           tokens.  Lane (rg, cl) has the logits of tokens 4 rg .. + 3 of both pages and loads just those tokens' values.
 template <int DT, int G>
-__global__ __launch_bounds__(256, 3) void packed_kernel(KvView kv, const uint8_t *__restrict__ q, int window, int num_sinks,
-                                                        int nsplit, float *__restrict__ partial, float *__restrict__ out,
+__global__ __launch_bounds__(256, 3) void packed_kernel(KvView kv, const uint8_t *__restrict__ q, SplitPlan plan,
+                                                        float *__restrict__ partial, float *__restrict__ out,
                                                         float *__restrict__ lse, int32_t *header) {
     constexpr int kRows = kRowsPerHead<G>;
     __shared__ __attribute__((aligned(16))) WaveSums<G> sums;
     const int tid = threadIdx.x, lane = tid & 63, rg = lane >> 4, cl = lane & 15;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);     // (so that table entries and page addresses are scalars)
     int wg = blockIdx.x;
-    if (nsplit == 1 && wg-- == 0) {
-        check_tables(kv, window, num_sinks, header, &sums.err[0]);
+    if (plan.checked && wg-- == 0) {
+        check_tables(kv, plan.window, plan.num_sinks, plan.blocks, header, &sums.err[0]);
         return;
     }
-    const int s = wg / nsplit, split = wg % nsplit, r = s / kv.num_kv_heads, h = s % kv.num_kv_heads;
-    if (nsplit > 1 && wg == 0 && tid < 64) header[tid] = 0;
+    const int s = wg / plan.nsplit, split = wg % plan.nsplit, r = s / kv.num_kv_heads, h = s % kv.num_kv_heads;
+    if (plan.nsplit > 1 && wg == 0 && tid < 64) header[tid] = 0;
     const int raw_ctx = kv.ctx_lens[r], ctx = ctx_clamped_quiet(kv, r);
     int err = raw_ctx != ctx ? PSA_DEVERR_CTX_RANGE : 0;
-    const Visible vis = make_visible(ctx, window, num_sinks);
-    const int per = (vis.count + nsplit - 1) / nsplit, b0 = split * per, b1 = min(vis.count, b0 + per);
+    const Visible vis = make_visible(ctx, plan.window, plan.num_sinks);
+    const int per = split_blocks(plan, vis.count), b0 = split * per, b1 = min(vis.count, b0 + per);
+    if (split > 0 && b0 >= vis.count) return;            // (the first split has a result even of no blocks)
 
     const int hd = cl / kRows, part = cl % kRows;
     const WeightParts<1, G> parts(part);
@@ -245,22 +245,21 @@ __global__ __launch_bounds__(256, 3) void packed_kernel(KvView kv, const uint8_t
     for (int t = 0; t < 8; ++t) acc[t] = f32x4_t{0.0f, 0.0f, 0.0f, 0.0f};
 
     const int32_t *table = kv.block_table + (size_t)r * kv.max_blocks;
-    auto load_block = [&](int b) __attribute__((always_inline)) {
-        const int page = table[vis.block(min(b, b1 - 1))], at = clamp_page_quiet(page, kv.num_pages);
-        if (page != at) err |= PSA_DEVERR_PAGE_RANGE;
-        return load_packed(kv.k_pool + ((size_t)at * kv.num_kv_heads + h) * kPackedBytes, lane);
-    };
-    PackedPage next[2];
-    if (b0 + 2 * wave < b1) {
-        next[0] = load_block(b0 + 2 * wave);
-        next[1] = load_block(b0 + 2 * wave + 1);
-    }
-    for (int b = b0 + 2 * wave; b < b1; b += 8) {
-        PackedPage pg[2] = {next[0], next[1]};
-        if (b + 8 < b1) {                                // the next pair is under way while this one is worked on
-            next[0] = load_block(b + 8);
-            next[1] = load_block(b + 9);
+    // Lane j holds the page of the j-th block of the wave's next 64 (32 pairs); the list after it is under way.
+    auto list_of = [&](int b) __attribute__((always_inline)) { return table[vis.block(min(b + 8 * (lane >> 1) + (lane & 1), b1 - 1))]; };
+    int pages = 0, later = 0;
+    auto load_pair = [&](PackedPage (&x)[2], int b, int i) __attribute__((always_inline)) {      // the wave's i-th pair
+        if ((i & 31) == 0) {
+            const int page = i == 0 ? list_of(b) : later;
+            pages = clamp_page_quiet(page, kv.num_pages);
+            if (pages != page) err |= PSA_DEVERR_PAGE_RANGE;
+            later = list_of(b + 256);
         }
+#pragma unroll
+        for (int y = 0; y < 2; ++y)
+            x[y] = load_packed(kv.k_pool + ((size_t)__builtin_amdgcn_readlane(pages, 2 * (i & 31) + y) * kv.num_kv_heads + h) * kPackedBytes, lane);
+    };
+    auto attend_pair = [&](PackedPage (&pg)[2], int b) __attribute__((always_inline)) {
         float sc[8];                                     // (not yet scaled)
 #pragma unroll
         for (int y = 0; y < 2; ++y) {
@@ -296,20 +295,36 @@ __global__ __launch_bounds__(256, 3) void packed_kernel(KvView kv, const uint8_t
 #pragma unroll
         for (int y = 0; y < kProducts<1, G>; ++y)
             a[y] = make_uint4(parts(p[0], p[1], y), parts(p[2], p[3], y), parts(p[4], p[5], y), parts(p[6], p[7], y));
-        uint4 vv[8];                                     // [page][token]: eight channels in bfloat16
+        float power[8];
 #pragma unroll
-        for (int y = 0; y < 2; ++y)
+        for (int j = 0; j < 8; ++j) power[j] = power_of((pg[j >> 2].vp >> (8 * (j & 3))) & 0xffu);
+        static_for<4>([&](auto u) __attribute__((always_inline)) {      // channels 2 u and 2 u + 1 of the lane's eight
+            uint32_t x[8];
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
-                vv[4 * y + j] = from_elements<1>(word_of(pg[y].v, j), power_of((pg[y].vp >> (8 * j)) & 0xffu));
-        static_for<8>([&](auto t) __attribute__((always_inline)) {
-            constexpr int w = t / 2;
-            constexpr bool odd = t & 1;
-            const uint4 bv = make_uint4(pick_halves<odd>(word_of(vv[0], w), word_of(vv[1], w)), pick_halves<odd>(word_of(vv[2], w), word_of(vv[3], w)),
-                                        pick_halves<odd>(word_of(vv[4], w), word_of(vv[5], w)), pick_halves<odd>(word_of(vv[6], w), word_of(vv[7], w)));
+            for (int j = 0; j < 8; ++j)
+                x[j] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(word_of(pg[j >> 2].v, j & 3), power[j], u));
+            const uint4 even = make_uint4(pick_halves<false>(x[0], x[1]), pick_halves<false>(x[2], x[3]), pick_halves<false>(x[4], x[5]), pick_halves<false>(x[6], x[7]));
+            const uint4 odd = make_uint4(pick_halves<true>(x[0], x[1]), pick_halves<true>(x[2], x[3]), pick_halves<true>(x[4], x[5]), pick_halves<true>(x[6], x[7]));
 #pragma unroll
-            for (int y = 0; y < kProducts<1, G>; ++y) acc[t] = mfma_16x16x32<1>(a[y], bv, acc[t]);
+            for (int y = 0; y < kProducts<1, G>; ++y) {
+                acc[2 * u] = mfma_16x16x32<1>(a[y], even, acc[2 * u]);
+                acc[2 * u + 1] = mfma_16x16x32<1>(a[y], odd, acc[2 * u + 1]);
+            }
         });
+    };
+    // The next pair is under way while one is worked on, in two sets of registers that take turns.  Loads beyond the last block
+    // read that one again, so that no branch hides from the compiler how many are outstanding.
+    PackedPage x0[2], x1[2];
+    const int first = b0 + 2 * wave;
+    if (first < b1) {
+        load_pair(x0, first, 0);
+        for (int b = first, i = 0; b < b1; b += 16, i += 2) {
+            load_pair(x1, b + 8, i + 1);
+            attend_pair(x0, b);
+            if (b + 8 >= b1) break;
+            load_pair(x0, b + 16, i + 2);
+            attend_pair(x1, b + 8);
+        }
     }
     l += __shfl_xor(l, 16);
     l += __shfl_xor(l, 32);
@@ -317,10 +332,11 @@ __global__ __launch_bounds__(256, 3) void packed_kernel(KvView kv, const uint8_t
     if (rg == 0 && hd < G && part == 0) { sums.m[wave][hd] = limit == -INFINITY ? -INFINITY : ref; sums.l[wave][hd] = l; }
     const bool bad_ctx = __ballot(err & PSA_DEVERR_CTX_RANGE) != 0ull, bad_page = __ballot(err & PSA_DEVERR_PAGE_RANGE) != 0ull;
     if (lane == 0) sums.err[wave] = (bad_ctx ? PSA_DEVERR_CTX_RANGE : 0) | (bad_page ? PSA_DEVERR_PAGE_RANGE : 0);
+    if (plan.nsplit == 1 && !plan.checked && sums.err[wave] && lane == 0) set_error(header, sums.err[wave]);
     __syncthreads();
     const size_t row = (size_t)r * kv.num_q_heads + h * G;
-    join_waves<G>(sums, tid, nsplit == 1, out + row * kHeadDim, lse ? lse + row : nullptr,
-                  partial + ((size_t)s * nsplit + split) * G * kSplitStride);
+    join_waves<G>(sums, tid, plan.nsplit == 1, out + row * kHeadDim, lse ? lse + row : nullptr,
+                  partial + ((size_t)s * plan.nsplit + split) * G * kSplitStride);
 }
 
 // ---- host side ----------------------------------------------------------------------------------
@@ -352,21 +368,22 @@ hipError_t launch_append_packed(const psa_kv_desc *d, void *packed, const void *
     return hipGetLastError();
 }
 
-constexpr int kPackedLeastBlocks = 16;
+constexpr int kPackedGroups = 768, kPackedLeastBlocks = 32;
 
 size_t packed_workspace_bytes(const psa_kv_desc *d, int window, int num_sinks) {
-    return visible_workspace_bytes(d, visible_plan(d, window, num_sinks, kPackedLeastBlocks));
+    return visible_workspace_bytes(d, visible_plan(d, window, num_sinks, kPackedGroups, kPackedLeastBlocks));
 }
 
 template <int DT, int G>
-static hipError_t launch_packed_t(const KvView &kv, const void *q, int window, int num_sinks, int nsplit, float *out, float *lse,
-                                  void *ws, hipStream_t st) {
+static hipError_t launch_packed_t(const KvView &kv, const void *q, const SplitPlan &plan, float *out, float *lse, void *ws,
+                                  hipStream_t st) {
     int32_t *header = reinterpret_cast<int32_t *>(ws);
     float *partial = reinterpret_cast<float *>(reinterpret_cast<uint8_t *>(ws) + 256);
-    const unsigned grid = (unsigned)(kv.batch * kv.num_kv_heads * nsplit + (nsplit == 1));
-    packed_kernel<DT, G><<<grid, 256, 0, st>>>(kv, (const uint8_t *)q, window, num_sinks, nsplit, partial, out, lse, header);
+    const unsigned grid = (unsigned)(kv.batch * kv.num_kv_heads * plan.nsplit + plan.checked);
+    if (plan.nsplit == 1 && !plan.checked && launch_clear(header, st) != hipSuccess) return hipErrorLaunchFailure;
+    packed_kernel<DT, G><<<grid, 256, 0, st>>>(kv, (const uint8_t *)q, plan, partial, out, lse, header);
     hipError_t e = hipGetLastError();
-    if (e == hipSuccess && nsplit > 1) e = launch_join(kv, G, nsplit, partial, out, lse, header, st);
+    if (e == hipSuccess && plan.nsplit > 1) e = launch_join(kv, plan, partial, out, lse, header, st);
     return e;
 }
 
@@ -381,9 +398,10 @@ hipError_t launch_packed(const psa_kv_desc *d, const void *packed, const void *q
         a.lse_out = lse;
         return launch_no_pages(kv, a, reinterpret_cast<int32_t *>(ws), st);
     }
-    const int G = d->num_q_heads / d->num_kv_heads, nsplit = visible_plan(d, window, num_sinks, kPackedLeastBlocks).nsplit;
+    const int G = d->num_q_heads / d->num_kv_heads;
+    const SplitPlan plan = visible_plan(d, window, num_sinks, kPackedGroups, kPackedLeastBlocks);
 #define PSA_CASE(DT, GG) \
-    if (d->dtype == DT && G == GG) return launch_packed_t<DT, GG>(kv, q, window, num_sinks, nsplit, out, lse, ws, st);
+    if (d->dtype == DT && G == GG) return launch_packed_t<DT, GG>(kv, q, plan, out, lse, ws, st);
     PSA_CASE(0, 1) PSA_CASE(0, 2) PSA_CASE(0, 4) PSA_CASE(0, 8)
     PSA_CASE(1, 1) PSA_CASE(1, 2) PSA_CASE(1, 4) PSA_CASE(1, 8)
 #undef PSA_CASE

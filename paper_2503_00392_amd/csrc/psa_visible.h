@@ -184,34 +184,42 @@ __device__ __forceinline__ void join_waves(const WaveSums<G> &w, int tid, bool d
     }
 }
 
-// Bits of the error word that a request's own workgroups find: one workgroup looks at every visible table entry of the call
-// and stores the word, where no launch follows that could do it.  (Each entry stands for a page that the other workgroups
-// read whole, so it is done before them.)
-__device__ __forceinline__ void check_tables(const KvView &kv, int window, int num_sinks, int32_t *header, int *shared_err) {
+// The error word where no launch follows that could collect it: one workgroup looks at every length and every visible table
+// entry of the call (`blocks` of a request at most) and stores the word, so that nobody has to clear it first.  It has
+// read them before the others have read the pages, as long as there are few: beyond kCheckedEntries the word is cleared by
+// a launch of its own, and whoever finds something sets it.
+constexpr int kCheckedEntries = 8192;
+__device__ __forceinline__ void check_tables(const KvView &kv, int window, int num_sinks, int blocks, int32_t *header, int *shared_err) {
     if (threadIdx.x == 0) *shared_err = 0;
     __syncthreads();
     int err = 0;
-    for (int r = threadIdx.x >> 6; r < kv.batch; r += blockDim.x >> 6) {
-        const int ctx = ctx_clamped_quiet(kv, r);
-        if (ctx != kv.ctx_lens[r]) err |= PSA_DEVERR_CTX_RANGE;
+    const int total = kv.batch * max(blocks, 1);
+#pragma unroll 8
+    for (int x = threadIdx.x; x < total; x += 256) {
+        const int r = x / max(blocks, 1), i = x % max(blocks, 1), ctx = ctx_clamped_quiet(kv, r);
         const Visible vis = make_visible(ctx, window, num_sinks);
-        const int32_t *table = kv.block_table + (size_t)r * kv.max_blocks;
-#pragma unroll 4
-        for (int i = threadIdx.x & 63; i < vis.count; i += 64)
-            if ((unsigned)table[vis.block(i)] >= (unsigned)kv.num_pages) err |= PSA_DEVERR_PAGE_RANGE;
+        const int page = kv.block_table[(size_t)r * kv.max_blocks + (i < vis.count ? vis.block(i) : 0)];
+        err |= (ctx != kv.ctx_lens[r] ? PSA_DEVERR_CTX_RANGE : 0) |
+               (i < vis.count && (unsigned)page >= (unsigned)kv.num_pages ? PSA_DEVERR_PAGE_RANGE : 0);
     }
     if (err) atomicOr(shared_err, err);
     __syncthreads();
     if (threadIdx.x < 64) header[threadIdx.x] = threadIdx.x == 1 ? *shared_err : 0;
 }
 
-// How a call is cut: blocks of a request that may be visible at most, splits of a request.
+// How a call is cut: a request's visible blocks into nsplit splits at most, of `least` blocks at least.
 struct SplitPlan {
-    int blocks, nsplit;
+    int window, num_sinks, nsplit, least, blocks;        // blocks: visible ones of a request at most
+    bool checked;                                        // one split, and few enough table entries for check_tables
 };
-SplitPlan visible_plan(const psa_kv_desc *d, int window, int num_sinks, int least_blocks);
+// Blocks of one split (but the last) of a request.
+__device__ __forceinline__ int split_blocks(const SplitPlan &p, int count) { return max((count + p.nsplit - 1) / p.nsplit, p.least); }
+
+// groups: workgroups that fill the GPU.
+SplitPlan visible_plan(const psa_kv_desc *d, int window, int num_sinks, int groups, int least_blocks);
 size_t visible_workspace_bytes(const psa_kv_desc *d, const SplitPlan &p);
-hipError_t launch_join(const KvView &kv, int G, int nsplit, const float *partial, float *out, float *lse, int32_t *header,
+hipError_t launch_clear(int32_t *header, hipStream_t st);
+hipError_t launch_join(const KvView &kv, const SplitPlan &plan, const float *partial, float *out, float *lse, int32_t *header,
                        hipStream_t st);
 
 }  // namespace psa
