@@ -26,8 +26,9 @@ struct RotateArgs {
     float eps;
 };
 
+typedef unsigned int u32x2_t __attribute__((ext_vector_type(2)));
 template <int DT>
-__device__ __forceinline__ void widen(const uint2 &w, float *x) {
+__device__ __forceinline__ void widen(const u32x2_t &w, float *x) {
     x[0] = cvt_lo<DT>(w.x); x[1] = cvt_hi<DT>(w.x); x[2] = cvt_lo<DT>(w.y); x[3] = cvt_hi<DT>(w.y);
 }
 template <int DT>
@@ -64,14 +65,15 @@ __global__ __launch_bounds__(256) void rotate_kernel(RotateArgs a) {
             sincospif(2.0f * t, &s[j], &c[j]);
         }
     }
-    for (int row = first + rg; row < last; row += 4) {
+    // what streams through is marked read (written) once
+    auto load = [&](int row, float (&x)[8]) __attribute__((always_inline)) {
+        const uint8_t *src = row < a.q_heads ? a.q_in + token * a.q_in_stride + row * kRowBytes
+                                             : a.k_in + token * a.k_in_stride + (row - a.q_heads) * kRowBytes;
+        widen<DT>(__builtin_nontemporal_load(reinterpret_cast<const u32x2_t *>(src + 2 * lo)), x);
+        widen<DT>(__builtin_nontemporal_load(reinterpret_cast<const u32x2_t *>(src + 2 * hi)), x + 4);
+    };
+    auto finish = [&](int row, float (&x)[8]) __attribute__((always_inline)) {
         const bool is_q = row < a.q_heads;
-        const int head = is_q ? row : row - a.q_heads;
-        const uint8_t *src = (is_q ? a.q_in + token * a.q_in_stride : a.k_in + token * a.k_in_stride) + head * kRowBytes;
-        uint8_t *dst = (is_q ? a.q_out + token * a.q_out_stride : a.k_out + token * a.k_out_stride) + head * kRowBytes;
-        float x[8];
-        widen<DT>(*reinterpret_cast<const uint2 *>(src + 2 * lo), x);
-        widen<DT>(*reinterpret_cast<const uint2 *>(src + 2 * hi), x + 4);
         if (a.normalize) {
             float sum = 0.0f;
 #pragma unroll
@@ -80,8 +82,8 @@ __global__ __launch_bounds__(256) void rotate_kernel(RotateArgs a) {
             const uint8_t *w = is_q ? a.q_weight : a.k_weight;
             float g[8] = {1.0f, 1.0f, 1.0f, 1.0f, 1.0f, 1.0f, 1.0f, 1.0f};
             if (w) {
-                widen<DT>(*reinterpret_cast<const uint2 *>(w + 2 * lo), g);
-                widen<DT>(*reinterpret_cast<const uint2 *>(w + 2 * hi), g + 4);
+                widen<DT>(*reinterpret_cast<const u32x2_t *>(w + 2 * lo), g);
+                widen<DT>(*reinterpret_cast<const u32x2_t *>(w + 2 * hi), g + 4);
             }
 #pragma unroll
             for (int j = 0; j < 8; ++j) x[j] = x[j] * f * g[j];
@@ -94,10 +96,22 @@ __global__ __launch_bounds__(256) void rotate_kernel(RotateArgs a) {
             y[u] = turned ? x[u] * c[j] - x[v] * s[j] : x[u];
             y[v] = turned ? x[u] * s[j] + x[v] * c[j] : x[v];
         }
-        *reinterpret_cast<uint2 *>(dst + 2 * lo) = make_uint2(round16<DT>(y[0], y[1]), round16<DT>(y[2], y[3]));
-        *reinterpret_cast<uint2 *>(dst + 2 * hi) = make_uint2(round16<DT>(y[4], y[5]), round16<DT>(y[6], y[7]));
+        uint8_t *dst = is_q ? a.q_out + token * a.q_out_stride + row * kRowBytes
+                            : a.k_out + token * a.k_out_stride + (row - a.q_heads) * kRowBytes;
+        __builtin_nontemporal_store(u32x2_t{round16<DT>(y[0], y[1]), round16<DT>(y[2], y[3])}, reinterpret_cast<u32x2_t *>(dst + 2 * lo));
+        __builtin_nontemporal_store(u32x2_t{round16<DT>(y[4], y[5]), round16<DT>(y[6], y[7])}, reinterpret_cast<u32x2_t *>(dst + 2 * hi));
+    };
+    for (int row = first + rg; row < last; row += 8) {   // two rows' loads before either's stores: both may be in place
+        float x[2][8];
+        const bool second = row + 4 < last;
+        load(row, x[0]);
+        if (second) load(row + 4, x[1]);
+        finish(row, x[0]);
+        if (second) finish(row + 4, x[1]);
     }
 }
+
+constexpr int kRotateWaves = 4096;
 
 hipError_t launch_rotate(const psa_rotate_desc *d, const void *q_in, const void *k_in, void *q_out, void *k_out, const void *q_weight,
                          const void *k_weight, const int32_t *positions, const float *inv_freq, hipStream_t st) {
@@ -120,9 +134,12 @@ hipError_t launch_rotate(const psa_rotate_desc *d, const void *q_in, const void 
     a.half = d->rot_dim / 2;
     a.normalize = d->normalize;
     a.eps = d->eps;
-    const int rows = a.q_heads + a.kv_heads;
-    a.rows_per_wave = rows;
-    a.waves_per_token = (rows + a.rows_per_wave - 1) / a.rows_per_wave;
+    // a wave takes all rows of its token where there are tokens enough to fill the GPU; fewer, down to four, where there are not
+    const int quads = (a.q_heads + a.kv_heads + 3) / 4;
+    const int want = a.tokens >= kRotateWaves ? 1 : (kRotateWaves + a.tokens - 1) / a.tokens, most = want < quads ? want : quads;
+    const int per_wave = (quads + most - 1) / most;
+    a.rows_per_wave = 4 * per_wave;
+    a.waves_per_token = (quads + per_wave - 1) / per_wave;
     const long long waves = (long long)a.tokens * a.waves_per_token;
     const unsigned grid = (unsigned)((waves + 3) / 4);
     auto kernel = d->dtype == PSA_F16 ? (d->interleaved ? rotate_kernel<0, true> : rotate_kernel<0, false>)
