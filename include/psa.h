@@ -304,9 +304,11 @@ psa_status psa_dense_attention(const psa_kv_desc *desc, const void *q, float *ou
  *        logits, may be NULL.  Where nothing is visible out = 0 and lse = -inf; a NaN in a visible key or value shows in the
  *        outputs of its heads
  *   workspace  psa_window_workspace_bytes of the same descriptor, window and num_sinks; holds the sticky error word
+ * A call repeated gives the same bits.  How a request is cut, and with it the order of its sums, follows from the lengths of all
+ * requests of the batch: its results can differ in the last bits from those it has in another batch.
  * Pages without a visible token are not looked at, nor are their block-table entries: they may have been freed.  What a
  * page holds beside the visible tokens does not matter (NaN included).
- * Shapes as for psa_dense_attention, max_blocks_per_seq up to 2^27 - 1; q 16-byte aligned.  With a second tier slices are read
+ * Shapes as for psa_dense_attention, max_blocks_per_seq up to 2^27 - 1; q and workspace 16-byte aligned.  With a second tier slices are read
  * from where the pools are.
  */
 size_t psa_window_workspace_bytes(const psa_kv_desc *desc, int32_t window, int32_t num_sinks);

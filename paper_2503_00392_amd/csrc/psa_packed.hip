@@ -198,25 +198,28 @@ __device__ __forceinline__ uint32_t word_of(const uint4 &v, int w) { return w ==
 //   values  D[row][channel] += P[row][token] V[token][channel], one 16x16x32 product for eight channels of the pair's 32
 //           tokens.  Lane (rg, cl) has the logits of tokens 4 rg .. + 3 of both pages and loads just those tokens' values.
 template <int DT, int G>
-__global__ __launch_bounds__(256, 3) void packed_kernel(KvView kv, const uint8_t *__restrict__ q, SplitPlan plan,
-                                                        float *__restrict__ partial, float *__restrict__ out,
-                                                        float *__restrict__ lse, int32_t *header) {
+__global__ __launch_bounds__(256, 3) void packed_kernel(KvView kv, const uint8_t *__restrict__ q, VisiblePlan plan,
+                                                        VisibleWs ws, float *__restrict__ out, float *__restrict__ lse) {
     constexpr int kRows = kRowsPerHead<G>;
     __shared__ __attribute__((aligned(16))) WaveSums<G> sums;
     const int tid = threadIdx.x, lane = tid & 63, rg = lane >> 4, cl = lane & 15;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);     // (so that table entries and page addresses are scalars)
     int wg = blockIdx.x;
     if (plan.checked && wg-- == 0) {
-        check_tables(kv, plan.window, plan.num_sinks, plan.blocks, header, &sums.err[0]);
+        check_tables(kv, plan.window, plan.num_sinks, plan.blocks, ws.header, &sums.err[0]);
         return;
     }
-    const int s = wg / plan.nsplit, split = wg % plan.nsplit, r = s / kv.num_kv_heads, h = s % kv.num_kv_heads;
-    if (plan.nsplit > 1 && wg == 0 && tid < 64) header[tid] = 0;
-    const int raw_ctx = kv.ctx_lens[r], ctx = ctx_clamped_quiet(kv, r);
+    const int h = wg % kv.num_kv_heads, u = wg / kv.num_kv_heads;       // all of request u, or piece u
+    Piece piece{u, 0, 0, true};
+    if (!plan.direct) {
+        __shared__ PieceShared shared_piece;
+        piece = find_piece(kv, plan, (uint32_t)u, wg == 0, ws, shared_piece);
+        if (piece.r >= kv.batch) return;
+    }
+    const int r = piece.r, raw_ctx = kv.ctx_lens[r], ctx = ctx_clamped_quiet(kv, r);
     int err = raw_ctx != ctx ? PSA_DEVERR_CTX_RANGE : 0;
     const Visible vis = make_visible(ctx, plan.window, plan.num_sinks);
-    const int per = split_blocks(plan, vis.count), b0 = split * per, b1 = min(vis.count, b0 + per);
-    if (split > 0 && b0 >= vis.count) return;            // (the first split has a result even of no blocks)
+    const int b0 = piece.b0, b1 = plan.direct ? vis.count : piece.b1;
 
     const int hd = cl / kRows, part = cl % kRows;
     const WeightParts<1, G> parts(part);
@@ -332,11 +335,11 @@ __global__ __launch_bounds__(256, 3) void packed_kernel(KvView kv, const uint8_t
     if (rg == 0 && hd < G && part == 0) { sums.m[wave][hd] = limit == -INFINITY ? -INFINITY : ref; sums.l[wave][hd] = l; }
     const bool bad_ctx = __ballot(err & PSA_DEVERR_CTX_RANGE) != 0ull, bad_page = __ballot(err & PSA_DEVERR_PAGE_RANGE) != 0ull;
     if (lane == 0) sums.err[wave] = (bad_ctx ? PSA_DEVERR_CTX_RANGE : 0) | (bad_page ? PSA_DEVERR_PAGE_RANGE : 0);
-    if (plan.nsplit == 1 && !plan.checked && sums.err[wave] && lane == 0) set_error(header, sums.err[wave]);
+    if (plan.direct && !plan.checked && sums.err[wave] && lane == 0) set_error(ws.header, sums.err[wave]);
     __syncthreads();
     const size_t row = (size_t)r * kv.num_q_heads + h * G;
-    join_waves<G>(sums, tid, plan.nsplit == 1, out + row * kHeadDim, lse ? lse + row : nullptr,
-                  partial + ((size_t)s * plan.nsplit + split) * G * kSplitStride);
+    join_waves<G>(sums, tid, piece.whole, out + row * kHeadDim, lse ? lse + row : nullptr,
+                  plan.direct ? nullptr : ws.records + (size_t)wg * G * kSplitStride);
 }
 
 // ---- host side ----------------------------------------------------------------------------------
@@ -368,23 +371,24 @@ hipError_t launch_append_packed(const psa_kv_desc *d, void *packed, const void *
     return hipGetLastError();
 }
 
-constexpr int kPackedGroups = 768, kPackedLeastBlocks = 32;
+// (measured: see the comment at the kernel)
+constexpr int kPackedGroups = 768, kPackedLeastBlocks = 32, kPackedDirectBlocks = 128;
+static VisiblePlan packed_plan(const psa_kv_desc *d, int window, int num_sinks) {
+    return visible_plan(d, window, num_sinks, kPackedGroups, kPackedLeastBlocks, kPackedDirectBlocks);
+}
 
 size_t packed_workspace_bytes(const psa_kv_desc *d, int window, int num_sinks) {
-    return visible_workspace_bytes(d, visible_plan(d, window, num_sinks, kPackedGroups, kPackedLeastBlocks));
+    return visible_workspace_bytes(d, packed_plan(d, window, num_sinks));
 }
 
 template <int DT, int G>
-static hipError_t launch_packed_t(const KvView &kv, const void *q, const SplitPlan &plan, float *out, float *lse, void *ws,
+static hipError_t launch_packed_t(const KvView &kv, const void *q, const VisiblePlan &plan, const VisibleWs &ws, float *out, float *lse,
                                   hipStream_t st) {
-    int32_t *header = reinterpret_cast<int32_t *>(ws);
-    float *partial = reinterpret_cast<float *>(reinterpret_cast<uint8_t *>(ws) + 256);
-    const unsigned grid = (unsigned)(kv.batch * kv.num_kv_heads * plan.nsplit + plan.checked);
-    if (plan.nsplit == 1 && !plan.checked && launch_clear(header, st) != hipSuccess) return hipErrorLaunchFailure;
-    packed_kernel<DT, G><<<grid, 256, 0, st>>>(kv, (const uint8_t *)q, plan, partial, out, lse, header);
-    hipError_t e = hipGetLastError();
-    if (e == hipSuccess && plan.nsplit > 1) e = launch_join(kv, plan, partial, out, lse, header, st);
-    return e;
+    const unsigned grid = (unsigned)(kv.num_kv_heads * (plan.direct ? kv.batch : plan.groups + kv.batch) + plan.checked);
+    if (plan.direct && !plan.checked && launch_clear(ws.header, st) != hipSuccess) return hipErrorLaunchFailure;
+    packed_kernel<DT, G><<<grid, 256, 0, st>>>(kv, (const uint8_t *)q, plan, ws, out, lse);
+    const hipError_t e = hipGetLastError();
+    return e == hipSuccess && !plan.direct ? launch_join(kv, plan, ws, out, lse, st) : e;
 }
 
 hipError_t launch_packed(const psa_kv_desc *d, const void *packed, const void *q, int window, int num_sinks, float *out, float *lse,
@@ -399,9 +403,10 @@ hipError_t launch_packed(const psa_kv_desc *d, const void *packed, const void *q
         return launch_no_pages(kv, a, reinterpret_cast<int32_t *>(ws), st);
     }
     const int G = d->num_q_heads / d->num_kv_heads;
-    const SplitPlan plan = visible_plan(d, window, num_sinks, kPackedGroups, kPackedLeastBlocks);
+    const VisiblePlan plan = packed_plan(d, window, num_sinks);
+    const VisibleWs vws = visible_ws(d, ws);
 #define PSA_CASE(DT, GG) \
-    if (d->dtype == DT && G == GG) return launch_packed_t<DT, GG>(kv, q, plan, out, lse, ws, st);
+    if (d->dtype == DT && G == GG) return launch_packed_t<DT, GG>(kv, q, plan, vws, out, lse, st);
     PSA_CASE(0, 1) PSA_CASE(0, 2) PSA_CASE(0, 4) PSA_CASE(0, 8)
     PSA_CASE(1, 1) PSA_CASE(1, 2) PSA_CASE(1, 4) PSA_CASE(1, 8)
 #undef PSA_CASE

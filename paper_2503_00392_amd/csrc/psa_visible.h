@@ -1,14 +1,13 @@
 // What the two attention kernels with a window share (psa_window.hip over the 16-bit cache, psa_packed.hip over the 4-bit
-// one): which tokens a query sees, the weights of the value product in parts, and how the waves' and the splits' running
-// sums come together.
+// one): which tokens a query sees, the weights of the value product in parts, and how the work is cut and how
+// running sums come together.
 #pragma once
 
 #include "psa_attend.h"
 
 namespace psa {
 
-constexpr int kMaxSplits = 1024;      // splits of a request at most: their weights are an array in the merge's LDS
-constexpr int kSplitStride = 132;     // floats of one split's result for one head: M, l, error bits (head 0), pad, acc[128]
+constexpr int kSplitStride = 132;     // floats of one record for one head: M, l, error bits (head 0), pad, acc[128]
 
 // The query stands at position ctx - 1 and sees token t < ctx if t < sinks or t >= start = ctx - window.  The blocks that
 // hold a visible token are 0 .. head-1 and tail .. N-1, and only these are ever looked at: a table entry or a page between
@@ -153,7 +152,7 @@ __device__ __forceinline__ float joined_out(float n, float den) { return den == 
 __device__ __forceinline__ float joined_lse(float M, float den) { return den == 0.0f ? -INFINITY : (M + log2_fast(den)) * kLn2; }
 
 // The four waves of a workgroup, joined through LDS: rows[wave][head][channel] and the waves' maxima and sums.  Either the
-// request's results (one split) or the split's record.
+// request's results (`whole`) or a record; a record's error bits in any case.
 template <int G>
 struct WaveSums {
     float acc[4][G][kHeadDim];
@@ -161,8 +160,8 @@ struct WaveSums {
     int err[4];
 };
 template <int G>
-__device__ __forceinline__ void join_waves(const WaveSums<G> &w, int tid, bool direct, float *out, float *lse, float *record) {
-    if (!direct && tid == 0) record[2] = __int_as_float(w.err[0] | w.err[1] | w.err[2] | w.err[3]);
+__device__ __forceinline__ void join_waves(const WaveSums<G> &w, int tid, bool whole, float *out, float *lse, float *record) {
+    if (record && tid == 0) record[2] = __int_as_float(w.err[0] | w.err[1] | w.err[2] | w.err[3]);
     for (int idx = tid; idx < G * kHeadDim; idx += 256) {
         const int g = idx / kHeadDim, ch = idx % kHeadDim;
         const float M = fmaxf(fmaxf(w.m[0][g], w.m[1][g]), fmaxf(w.m[2][g], w.m[3][g]));
@@ -173,7 +172,7 @@ __device__ __forceinline__ void join_waves(const WaveSums<G> &w, int tid, bool d
             den += w.l[i][g] * f;
             num += w.acc[i][g][ch] * f;
         }
-        if (direct) {
+        if (whole) {
             out[g * kHeadDim + ch] = joined_out(num, den);
             if (lse && ch == 0) lse[g] = joined_lse(M, den);
         } else {
@@ -207,19 +206,114 @@ __device__ __forceinline__ void check_tables(const KvView &kv, int window, int n
     if (threadIdx.x < 64) header[threadIdx.x] = threadIdx.x == 1 ? *shared_err : 0;
 }
 
-// How a call is cut: a request's visible blocks into nsplit splits at most, of `least` blocks at least.
-struct SplitPlan {
-    int window, num_sinks, nsplit, least, blocks;        // blocks: visible ones of a request at most
-    bool checked;                                        // one split, and few enough table entries for check_tables
+// How a call is cut.
+//   direct   a workgroup for every (request, KV head), which writes the results: where there are enough of them to fill the GPU
+//            and none has much to read.
+//   planned  workgroups take pieces of requests: a piece is what the visible blocks of all requests come to, divided by the
+//            workgroups that fill the GPU, and a request gets as many as it takes -- one long request among short ones is
+//            shared by many.  A piece's result is a record, unless it is all of its request, and a second launch joins the records of a request.  Every workgroup finds
+//            its piece from the lengths by itself; the first one also leaves the requests' first records for the launch that joins.
+// Few pieces, because what a workgroup does before its first block and after its last (dependent trips to memory, the
+// exchange between its waves) costs as much as twenty blocks: the same bytes in pieces of half the size and two
+// rounds of workgroups took 15 % longer.  So a request keeps one piece (or two, ...) up to a quarter more than these hold.
+struct VisiblePlan {
+    int window, num_sinks;
+    int blocks;                    // visible blocks of a request at most
+    int groups, least;             // planned: workgroups for a KV head that fill the GPU; blocks of a piece at least
+    bool direct, checked;          // checked: direct, and few enough table entries for check_tables
 };
-// Blocks of one split (but the last) of a request.
-__device__ __forceinline__ int split_blocks(const SplitPlan &p, int count) { return max((count + p.nsplit - 1) / p.nsplit, p.least); }
+VisiblePlan visible_plan(const psa_kv_desc *d, int window, int num_sinks, int groups, int least, int direct_blocks);
+size_t visible_workspace_bytes(const psa_kv_desc *d, const VisiblePlan &p);
 
-// groups: workgroups that fill the GPU.
-SplitPlan visible_plan(const psa_kv_desc *d, int window, int num_sinks, int groups, int least_blocks);
-size_t visible_workspace_bytes(const psa_kv_desc *d, const SplitPlan &p);
+// The workspace: header (word 1: error bits, word 2: length of a piece), the requests' first records, the records.
+struct VisibleWs {
+    int32_t *header;
+    uint32_t *first;               // [batch]
+    float *records;                // [groups + batch][num_kv_heads][G][kSplitStride]
+};
+VisibleWs visible_ws(const psa_kv_desc *d, void *ws);
 hipError_t launch_clear(int32_t *header, hipStream_t st);
-hipError_t launch_join(const KvView &kv, const SplitPlan &plan, const float *partial, float *out, float *lse, int32_t *header,
-                       hipStream_t st);
+hipError_t launch_join(const KvView &kv, const VisiblePlan &plan, const VisibleWs &ws, float *out, float *lse, hipStream_t st);
+
+__device__ __forceinline__ int visible_count(const KvView &kv, const VisiblePlan &plan, int r) {
+    return make_visible(ctx_clamped_quiet(kv, r), plan.window, plan.num_sinks).count;
+}
+
+// Pieces of a request of `count` visible blocks.
+__device__ __forceinline__ uint32_t pieces_of(uint32_t count, uint32_t length) {
+    const uint32_t over = length / 4;
+    return count == 0 ? 0u : (count <= over ? 1u : (count - over + length - 1) / length);
+}
+
+struct Piece {
+    int r, b0, b1;                 // r = batch: there is no such piece
+    bool whole;                    // all of its request
+};
+__device__ __forceinline__ Piece make_piece(int r, uint32_t at, uint32_t count, uint32_t n) {
+    const uint32_t per = (count + n - 1) / n;
+    return {r, (int)(at * per), (int)min(count, (at + 1) * per), n == 1};
+}
+// Length of a piece; the last one of a request is a quarter of a piece too short in the mean: that much is left for it.
+__device__ __forceinline__ uint32_t piece_length(const KvView &kv, const VisiblePlan &plan, uint32_t total) {
+    const uint32_t share = max(plan.groups - kv.batch / 4, (plan.groups + 1) / 2);
+    return max((total + share - 1) / share, (uint32_t)plan.least);
+}
+struct PieceShared {
+    uint32_t wave[4];
+    int r;
+    uint32_t at, count;            // which of the request's pieces, and its blocks
+};
+// Piece u.  256 threads; `leave`: this workgroup leaves the requests' first records and the length of a piece.
+__device__ __forceinline__ Piece find_piece(const KvView &kv, const VisiblePlan &plan, uint32_t u, bool leave, const VisibleWs &ws,
+                                            PieceShared &sh) {
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    if (kv.batch <= 64) {                                // every wave by itself, a lane for each request
+        const uint32_t count = lane < kv.batch ? (uint32_t)visible_count(kv, plan, lane) : 0u;
+        const uint32_t length = piece_length(kv, plan, (uint32_t)__builtin_amdgcn_readlane((int)wave_prefix_sum(count), 63));
+        const uint32_t n = pieces_of(count, length), first = wave_prefix_sum(n) - n;
+        if (leave && lane < kv.batch) ws.first[lane] = first;
+        if (leave) ws.header[lane] = lane == 2 ? (int32_t)length : 0;
+        const unsigned long long hit = __ballot(u >= first && u < first + n);
+        if (!hit) return {kv.batch, 0, 0, false};
+        const int r = __builtin_ctzll(hit);
+        return make_piece(r, u - (uint32_t)__builtin_amdgcn_readlane((int)first, r), (uint32_t)__builtin_amdgcn_readlane((int)count, r),
+                          (uint32_t)__builtin_amdgcn_readlane((int)n, r));
+    }
+    const uint32_t mine = tid < kv.batch ? (uint32_t)visible_count(kv, plan, tid) : 0u;
+    uint32_t sum = mine;
+    for (int r = tid + 256; r < kv.batch; r += 256) sum += (uint32_t)visible_count(kv, plan, r);
+    sum = wave_prefix_sum(sum);
+    if (lane == 63) sh.wave[wave] = sum;
+    if (tid == 0) sh.r = kv.batch;
+    __syncthreads();
+    const uint32_t length = piece_length(kv, plan, sh.wave[0] + sh.wave[1] + sh.wave[2] + sh.wave[3]);
+    uint32_t before = 0;
+    for (int r0 = 0; r0 < kv.batch; r0 += 256) {
+        const int r = r0 + tid;
+        const uint32_t count = r0 == 0 ? mine : (r < kv.batch ? (uint32_t)visible_count(kv, plan, r) : 0u);
+        const uint32_t n = pieces_of(count, length), upto = wave_prefix_sum(n);
+        __syncthreads();                                 // (the sums of the step before have been read)
+        if (lane == 63) sh.wave[wave] = upto;
+        __syncthreads();
+        uint32_t first = before + upto - n;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            if (w < wave) first += sh.wave[w];
+            before += sh.wave[w];
+        }
+        if (leave && r < kv.batch) ws.first[r] = first;
+        if (u >= first && u < first + n) {
+            sh.r = r;
+            sh.at = u - first;
+            sh.count = count;
+        }
+    }
+    if (leave && tid < 64) ws.header[tid] = tid == 2 ? (int32_t)length : 0;
+    __syncthreads();
+    const int r = __builtin_amdgcn_readfirstlane(sh.r);
+    if (r >= kv.batch) return {r, 0, 0, false};
+    const uint32_t count = (uint32_t)__builtin_amdgcn_readfirstlane((int)sh.count);
+    return make_piece(r, (uint32_t)__builtin_amdgcn_readfirstlane((int)sh.at), count, pieces_of(count, length));
+}
 
 }  // namespace psa

@@ -12,9 +12,8 @@ namespace psa {
 // logits of the head of row n for tokens kq, 4+kq, 8+kq, 12+kq; values with eight 16x16x16 products, the weights in parts in
 // a head's rows.  Tokens of a block that the query does not see get the logit -inf and a zero value row (the page may hold NaN there).
 template <int DT, int G>
-__global__ __launch_bounds__(256, 3) void window_kernel(KvView kv, const uint8_t *__restrict__ q, SplitPlan plan,
-                                                        float *__restrict__ partial, float *__restrict__ out,
-                                                        float *__restrict__ lse, int32_t *header) {
+__global__ __launch_bounds__(256, 3) void window_kernel(KvView kv, const uint8_t *__restrict__ q, VisiblePlan plan,
+                                                        VisibleWs ws, float *__restrict__ out, float *__restrict__ lse) {
     constexpr int kRows = kRowsPerHead<G>;
     __shared__ uint4 stage[4][16 * 17];                  // per wave: a key slice on its way into the operand's layout
     __shared__ __attribute__((aligned(16))) WaveSums<G> sums;
@@ -22,16 +21,20 @@ __global__ __launch_bounds__(256, 3) void window_kernel(KvView kv, const uint8_t
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);     // (so that what hangs on it is a scalar)
     int wg = blockIdx.x;
     if (plan.checked && wg-- == 0) {
-        check_tables(kv, plan.window, plan.num_sinks, plan.blocks, header, &sums.err[0]);
+        check_tables(kv, plan.window, plan.num_sinks, plan.blocks, ws.header, &sums.err[0]);
         return;
     }
-    const int s = wg / plan.nsplit, split = wg % plan.nsplit, r = s / kv.num_kv_heads, h = s % kv.num_kv_heads;
-    if (plan.nsplit > 1 && wg == 0 && tid < 64) header[tid] = 0;      // the launch that joins the splits sets the error word
-    const int raw_ctx = kv.ctx_lens[r], ctx = ctx_clamped_quiet(kv, r);
+    const int h = wg % kv.num_kv_heads, u = wg / kv.num_kv_heads;       // all of request u, or piece u
+    Piece piece{u, 0, 0, true};
+    if (!plan.direct) {
+        __shared__ PieceShared shared_piece;
+        piece = find_piece(kv, plan, (uint32_t)u, wg == 0, ws, shared_piece);
+        if (piece.r >= kv.batch) return;
+    }
+    const int r = piece.r, raw_ctx = kv.ctx_lens[r], ctx = ctx_clamped_quiet(kv, r);
     int err = raw_ctx != ctx ? PSA_DEVERR_CTX_RANGE : 0;
     const Visible vis = make_visible(ctx, plan.window, plan.num_sinks);
-    const int per = split_blocks(plan, vis.count), b0 = split * per, b1 = min(vis.count, b0 + per);
-    if (split > 0 && b0 >= vis.count) return;            // (the first split has a result even of no blocks)
+    const int b0 = piece.b0, b1 = plan.direct ? vis.count : piece.b1;
 
     const int hd = cl / kRows, part = cl % kRows;
     const WeightParts<DT, G> parts(part);
@@ -105,63 +108,62 @@ __global__ __launch_bounds__(256, 3) void window_kernel(KvView kv, const uint8_t
     if (rg == 0 && hd < G && part == 0) { sums.m[wave][hd] = limit == -INFINITY ? -INFINITY : ref; sums.l[wave][hd] = l; }
     const bool bad_ctx = __ballot(err & PSA_DEVERR_CTX_RANGE) != 0ull, bad_page = __ballot(err & PSA_DEVERR_PAGE_RANGE) != 0ull;
     if (lane == 0) sums.err[wave] = (bad_ctx ? PSA_DEVERR_CTX_RANGE : 0) | (bad_page ? PSA_DEVERR_PAGE_RANGE : 0);
-    if (plan.nsplit == 1 && !plan.checked && sums.err[wave] && lane == 0) set_error(header, sums.err[wave]);
+    if (plan.direct && !plan.checked && sums.err[wave] && lane == 0) set_error(ws.header, sums.err[wave]);
     __syncthreads();
     const size_t row = (size_t)r * kv.num_q_heads + h * G;
-    join_waves<G>(sums, tid, plan.nsplit == 1, out + row * kHeadDim, lse ? lse + row : nullptr,
-                  partial + ((size_t)s * plan.nsplit + split) * G * kSplitStride);
+    join_waves<G>(sums, tid, piece.whole, out + row * kHeadDim, lse ? lse + row : nullptr,
+                  plan.direct ? nullptr : ws.records + (size_t)wg * G * kSplitStride);
 }
 
-// grid (S * G); 512 threads = 16 split lanes x 32 quarters of a row.  Split lane j takes splits j, j + 16, ... in ascending
-// order, four rows under way -- the first four before the maximum over the splits is known, so that up to 64 splits cost one
-// trip to memory and not two; the sixteen are added in a fixed order.
-__global__ __launch_bounds__(512) void join_kernel(KvView kv, SplitPlan plan, const float *__restrict__ partial,
-                                                   float *__restrict__ out, float *__restrict__ lse, int32_t *header) {
-    __shared__ float red[8];
-    __shared__ f32x4_t num_part[16][32];
-    __shared__ float den_part[16];
-    const int G = kv.num_q_heads / kv.num_kv_heads, s = blockIdx.x / G, g = blockIdx.x % G, r = s / kv.num_kv_heads;
+// grid (batch * num_q_heads); LANES record lanes x 32 quarters of a row.  Lane j takes the request's records j, j + LANES, ... in
+// ascending order, four rows under way; the lanes are added in a fixed order.  A request in one piece has its results already.
+template <int LANES>
+__global__ __launch_bounds__(32 * LANES) void join_kernel(KvView kv, VisiblePlan plan, VisibleWs ws, float *__restrict__ out,
+                                                   float *__restrict__ lse) {
+    constexpr int kWaves = LANES / 2;
+    __shared__ float red[kWaves];
+    __shared__ f32x4_t num_part[LANES][32];
+    __shared__ float den_part[LANES];
+    const int G = kv.num_q_heads / kv.num_kv_heads, s = blockIdx.x / G, g = blockIdx.x % G, r = s / kv.num_kv_heads, h = s % kv.num_kv_heads;
     const int tid = threadIdx.x, quarter = tid & 31, sl = tid >> 5;
-    const float *src = partial + ((size_t)s * plan.nsplit * G + g) * kSplitStride;
-    const size_t stride = (size_t)G * kSplitStride;
+    const int ctx = ctx_clamped_quiet(kv, r), count = make_visible(ctx, plan.window, plan.num_sinks).count;
+    const uint32_t first = ws.first[r], n = pieces_of((uint32_t)count, (uint32_t)ws.header[2]);
+    const float *src = ws.records + (((size_t)first * kv.num_kv_heads + h) * G + g) * kSplitStride;
+    const size_t stride = (size_t)kv.num_kv_heads * G * kSplitStride;
     f32x4_t a[4];
     float m[4], l[4];
-    auto load = [&](int i0) __attribute__((always_inline)) {
+    auto load = [&](uint32_t i0) __attribute__((always_inline)) {
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-            const float *row = src + (size_t)min(i0 + 16 * k, plan.nsplit - 1) * stride;
+            const float *row = src + (size_t)min(i0 + LANES * k, n - 1) * stride;
             a[k] = *reinterpret_cast<const f32x4_t *>(row + 4 + 4 * quarter);
             m[k] = row[0];
             l[k] = row[1];
         }
     };
-    load(sl);                                            // (beyond the splits that have a result: not used)
-    const float *mine = src + (size_t)min(tid, plan.nsplit - 1) * stride;
-    float M = mine[0];
-    int err = __float_as_int(mine[2]);
-    const int count = make_visible(ctx_clamped_quiet(kv, r), plan.window, plan.num_sinks).count, per = split_blocks(plan, count);
-    const int nsplit = max(1, (count + per - 1) / per);  // splits that have a result
-    if (tid >= nsplit) {
-        M = -INFINITY;
-        err = 0;
-    }
-    for (int i = tid + 512; i < nsplit; i += 512) {
+    if (n > 1) load(sl);
+    float M = -INFINITY;
+    int err = ctx != kv.ctx_lens[r] ? PSA_DEVERR_CTX_RANGE : 0;
+    for (uint32_t i = tid; i < n; i += 32 * LANES) {
         M = fmaxf(M, src[i * stride]);
-        err |= __float_as_int(src[i * stride + 2]);
+        if (g == 0) err |= __float_as_int(src[i * stride + 2]);
     }
-    if (g == 0 && err) set_error(header, err);
+    if (err) set_error(ws.header, err);
+    if (n == 1) return;
 #pragma unroll
     for (int d = 32; d >= 1; d >>= 1) M = fmaxf(M, __shfl_xor(M, d));
     if ((tid & 63) == 0) red[tid >> 6] = M;
     __syncthreads();
-    M = fmaxf(fmaxf(fmaxf(red[0], red[1]), fmaxf(red[2], red[3])), fmaxf(fmaxf(red[4], red[5]), fmaxf(red[6], red[7])));
+    M = red[0];
+#pragma unroll
+    for (int w = 1; w < kWaves; ++w) M = fmaxf(M, red[w]);
     f32x4_t num = {0.0f, 0.0f, 0.0f, 0.0f};
     float den = 0.0f;
-    for (int i0 = sl; i0 < nsplit; i0 += 64) {
+    for (uint32_t i0 = sl; i0 < n; i0 += 4 * LANES) {
         if (i0 != sl) load(i0);
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-            if (i0 + 16 * k < nsplit) {
+            if (i0 + LANES * k < n) {
                 const float w = join_weight(m[k], M);
                 num += a[k] * w;
                 den = fmaf(l[k], w, den);
@@ -172,22 +174,22 @@ __global__ __launch_bounds__(512) void join_kernel(KvView kv, SplitPlan plan, co
     if (quarter == 0) den_part[sl] = den;
     __syncthreads();
     if (tid < kHeadDim) {
-        float n[16], d[16];
+        float nn[LANES], d[LANES];
 #pragma unroll
-        for (int j = 0; j < 16; ++j) {
-            n[j] = reinterpret_cast<const float *>(num_part[j])[tid];
+        for (int j = 0; j < LANES; ++j) {
+            nn[j] = reinterpret_cast<const float *>(num_part[j])[tid];
             d[j] = den_part[j];
         }
 #pragma unroll
-        for (int w = 8; w >= 1; w >>= 1) {
+        for (int w = LANES / 2; w >= 1; w >>= 1) {
 #pragma unroll
             for (int j = 0; j < w; ++j) {
-                n[j] += n[j + w];
+                nn[j] += nn[j + w];
                 d[j] += d[j + w];
             }
         }
         const size_t row = (size_t)s * G + g;            // = r * num_q_heads + h * G + g
-        out[row * kHeadDim + tid] = joined_out(n[0], d[0]);
+        out[row * kHeadDim + tid] = joined_out(nn[0], d[0]);
         if (lse && tid == 0) lse[row] = joined_lse(M, d[0]);
     }
 }
@@ -195,22 +197,31 @@ __global__ __launch_bounds__(512) void join_kernel(KvView kv, SplitPlan plan, co
 __global__ void clear_error_word_kernel(int32_t *header) { header[threadIdx.x] = 0; }
 
 // ---- host side ----------------------------------------------------------------------------------
-SplitPlan visible_plan(const psa_kv_desc *d, int window, int num_sinks, int groups, int least_blocks) {
-    const long long S = (long long)d->batch * d->num_kv_heads;
+VisiblePlan visible_plan(const psa_kv_desc *d, int window, int num_sinks, int groups, int least, int direct_blocks) {
+    const long long H = d->num_kv_heads, S = d->batch * H;
     // a window of w tokens lies in at most (w + 14) / 16 + 1 blocks
     const long long tail = window > 0 ? ((long long)window + 14) / kPage + 1 : 0, head = ((long long)num_sinks + kPage - 1) / kPage;
-    const long long blocks = head + tail < d->max_blocks_per_seq ? head + tail : d->max_blocks_per_seq;
-    const long long want = S > 0 ? (groups + S - 1) / S : 1, by_length = (blocks + least_blocks - 1) / least_blocks;
-    SplitPlan p{window, num_sinks, 1, least_blocks, (int)blocks, false};
-    p.nsplit = (int)(want < by_length ? want : by_length);
-    if (p.nsplit > kMaxSplits) p.nsplit = kMaxSplits;
-    if (p.nsplit < 1) p.nsplit = 1;
-    p.checked = p.nsplit == 1 && d->batch * (blocks > 0 ? blocks : 1) <= kCheckedEntries;
+    const long long blocks = head + tail < d->max_blocks_per_seq ? head + tail : d->max_blocks_per_seq, all = d->batch * blocks;
+    VisiblePlan p{window, num_sinks, (int)blocks, 1, least, false, false};
+    p.direct = blocks <= least || (2 * S >= groups && blocks <= direct_blocks) || all > INT32_MAX;
+    p.checked = p.direct && all <= kCheckedEntries * (H >= 4 ? 16 : 1);
+    if (!p.direct) {
+        const long long most = (all + least - 1) / least, want = (groups + H - 1) / H;
+        p.groups = (int)(want < most ? want : (most > 0 ? most : 1));
+    }
     return p;
 }
 
-size_t visible_workspace_bytes(const psa_kv_desc *d, const SplitPlan &p) {
-    return 256 + (p.nsplit > 1 ? (size_t)d->batch * d->num_q_heads * p.nsplit * kSplitStride * sizeof(float) : 0);
+static size_t first_bytes(const psa_kv_desc *d) { return ((size_t)d->batch * 4 + 255) / 256 * 256; }
+
+size_t visible_workspace_bytes(const psa_kv_desc *d, const VisiblePlan &p) {
+    if (p.direct) return 256;
+    return 256 + first_bytes(d) + (size_t)(d->batch + p.groups) * d->num_q_heads * kSplitStride * sizeof(float);
+}
+
+VisibleWs visible_ws(const psa_kv_desc *d, void *ws) {
+    uint8_t *base = static_cast<uint8_t *>(ws);
+    return {reinterpret_cast<int32_t *>(base), reinterpret_cast<uint32_t *>(base + 256), reinterpret_cast<float *>(base + 256 + first_bytes(d))};
 }
 
 hipError_t launch_clear(int32_t *header, hipStream_t st) {
@@ -218,29 +229,32 @@ hipError_t launch_clear(int32_t *header, hipStream_t st) {
     return hipGetLastError();
 }
 
-hipError_t launch_join(const KvView &kv, const SplitPlan &plan, const float *partial, float *out, float *lse, int32_t *header,
-                       hipStream_t st) {
-    join_kernel<<<kv.batch * kv.num_q_heads, 512, 0, st>>>(kv, plan, partial, out, lse, header);
+hipError_t launch_join(const KvView &kv, const VisiblePlan &plan, const VisibleWs &ws, float *out, float *lse, hipStream_t st) {
+    // many requests have few pieces each: smaller workgroups, of which more are resident
+    const int rows = kv.batch * kv.num_q_heads;
+    if (rows >= 1024) join_kernel<4><<<rows, 128, 0, st>>>(kv, plan, ws, out, lse);
+    else join_kernel<16><<<rows, 512, 0, st>>>(kv, plan, ws, out, lse);
     return hipGetLastError();
 }
 
-constexpr int kWindowGroups = 512, kWindowLeastBlocks = 4;
+// (measured: see the comment at the kernel)
+constexpr int kWindowGroups = 512, kWindowLeastBlocks = 4, kWindowDirectBlocks = 128;
+static VisiblePlan window_plan(const psa_kv_desc *d, int window, int num_sinks) {
+    return visible_plan(d, window, num_sinks, kWindowGroups, kWindowLeastBlocks, kWindowDirectBlocks);
+}
 
 size_t window_workspace_bytes(const psa_kv_desc *d, int window, int num_sinks) {
-    return visible_workspace_bytes(d, visible_plan(d, window, num_sinks, kWindowGroups, kWindowLeastBlocks));
+    return visible_workspace_bytes(d, window_plan(d, window, num_sinks));
 }
 
 template <int DT, int G>
-static hipError_t launch_window_t(const KvView &kv, const void *q, const SplitPlan &plan, float *out, float *lse, void *ws,
+static hipError_t launch_window_t(const KvView &kv, const void *q, const VisiblePlan &plan, const VisibleWs &ws, float *out, float *lse,
                                   hipStream_t st) {
-    int32_t *header = reinterpret_cast<int32_t *>(ws);
-    float *partial = reinterpret_cast<float *>(reinterpret_cast<uint8_t *>(ws) + 256);
-    const unsigned grid = (unsigned)(kv.batch * kv.num_kv_heads * plan.nsplit + plan.checked);
-    if (plan.nsplit == 1 && !plan.checked && launch_clear(header, st) != hipSuccess) return hipErrorLaunchFailure;
-    window_kernel<DT, G><<<grid, 256, 0, st>>>(kv, (const uint8_t *)q, plan, partial, out, lse, header);
-    hipError_t e = hipGetLastError();
-    if (e == hipSuccess && plan.nsplit > 1) e = launch_join(kv, plan, partial, out, lse, header, st);
-    return e;
+    const unsigned grid = (unsigned)(kv.num_kv_heads * (plan.direct ? kv.batch : plan.groups + kv.batch) + plan.checked);
+    if (plan.direct && !plan.checked && launch_clear(ws.header, st) != hipSuccess) return hipErrorLaunchFailure;
+    window_kernel<DT, G><<<grid, 256, 0, st>>>(kv, (const uint8_t *)q, plan, ws, out, lse);
+    const hipError_t e = hipGetLastError();
+    return e == hipSuccess && !plan.direct ? launch_join(kv, plan, ws, out, lse, st) : e;
 }
 
 hipError_t launch_window(const psa_kv_desc *d, const void *q, int window, int num_sinks, float *out, float *lse, void *ws,
@@ -253,9 +267,10 @@ hipError_t launch_window(const psa_kv_desc *d, const void *q, int window, int nu
         return launch_no_pages(kv, a, reinterpret_cast<int32_t *>(ws), st);
     }
     const int G = d->num_q_heads / d->num_kv_heads;
-    const SplitPlan plan = visible_plan(d, window, num_sinks, kWindowGroups, kWindowLeastBlocks);
+    const VisiblePlan plan = window_plan(d, window, num_sinks);
+    const VisibleWs vws = visible_ws(d, ws);
 #define PSA_CASE(DT, GG) \
-    if (d->dtype == DT && G == GG) return launch_window_t<DT, GG>(kv, q, plan, out, lse, ws, st);
+    if (d->dtype == DT && G == GG) return launch_window_t<DT, GG>(kv, q, plan, vws, out, lse, st);
     PSA_CASE(0, 1) PSA_CASE(0, 2) PSA_CASE(0, 4) PSA_CASE(0, 8)
     PSA_CASE(1, 1) PSA_CASE(1, 2) PSA_CASE(1, 4) PSA_CASE(1, 8)
 #undef PSA_CASE

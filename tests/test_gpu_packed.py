@@ -274,3 +274,20 @@ def test_repeats_bit_for_bit(psa):
     first = psa.packed_attention(kv, q)
     again = psa.packed_attention(kv, q)
     assert torch.equal(first[0], again[0]) and torch.equal(first[1], again[1])
+
+
+@pytest.mark.parametrize("B,H,G", [(5, 8, 4), (64, 2, 8), (65, 1, 1), (300, 3, 2)])
+def test_one_long_request_among_short_ones(psa, B, H, G):
+    lens = [(i * 31) % 97 for i in range(B)]
+    lens[B // 2], lens[-1] = 9000, 2307
+    small, _ = cache(psa, [16 * 64], H, 1, torch.float16, seed=B)
+    gen = torch.Generator(device="cuda").manual_seed(B)
+    table = torch.randint(0, small.pool.shape[0], (B, 563), generator=gen, device="cuda", dtype=torch.int32)
+    q = torch.randn((B, H * G, 128), generator=gen, device="cuda").half()
+    kv = psa.PackedCache(small.pool, table, torch.tensor(lens, dtype=torch.int32, device="cuda"), H * G, torch.float16)
+    for window, sinks in [(INT_MAX, 0), (2500, 100)]:
+        check(psa, kv, q, lens, window, sinks)
+    table[B // 2, 562] = small.pool.shape[0]
+    kv.ctx_lens[0] = -1
+    out, _ = psa.packed_attention(kv, q)
+    assert psa.read_device_error(out._workspace) == 3

@@ -186,3 +186,48 @@ def test_host_tier(psa):
     got = psa.window_attention(host, q, 64, 5)
     torch.cuda.synchronize()
     assert torch.equal(want[0], got[0]) and torch.equal(want[1], got[1])
+
+
+@pytest.mark.parametrize("B,H,G", [(5, 8, 4), (64, 2, 8), (65, 1, 1), (70, 5, 2), (256, 1, 4), (257, 3, 8), (600, 1, 4)])
+def test_one_long_request_among_short_ones(psa, B, H, G):
+    """Pieces: a long request is cut into many, the others are one each, some requests are empty; batches about the sizes where a
+    workgroup finds its piece in another way."""
+    lens = [(i * 31) % 97 for i in range(B)]
+    lens[B // 2], lens[-1] = 6000, 2307
+    kv, q = cache(psa, lens[:1], H, G, torch.bfloat16, seed=B, width=1)
+    gen = torch.Generator(device="cuda").manual_seed(B)
+    k, v = (torch.randn((700, H, 16, 128), generator=gen, device="cuda").bfloat16() for _ in range(2))
+    table = torch.randint(0, 700, (B, 375), generator=gen, device="cuda", dtype=torch.int32)
+    q = torch.randn((B, H * G, 128), generator=gen, device="cuda").bfloat16()
+    kv = psa.KvCache(k, v, table, torch.tensor(lens, dtype=torch.int32, device="cuda"), H * G)
+    for window, sinks in [(INT_MAX, 0), (2500, 100)]:
+        out, lse = check(psa, kv, q, lens, window, sinks)
+        again = psa.window_attention(kv, q, window, sinks)
+        assert torch.equal(out, again[0]) and torch.equal(lse, again[1])
+    table[B // 2, 374] = -1                                   # in the long one's last piece
+    kv.ctx_lens[0] = -1                                       # of a request without a piece
+    out, _ = psa.window_attention(kv, q, INT_MAX)
+    assert psa.read_device_error(out._workspace) == 3
+
+
+def test_so_many_requests_that_no_workgroup_checks_the_tables(psa):
+    B = 9000
+    gen = torch.Generator(device="cuda").manual_seed(3)
+    k, v = (torch.randn((50, 1, 16, 128), generator=gen, device="cuda").half() for _ in range(2))
+    table = torch.randint(0, 50, (B, 1), generator=gen, device="cuda", dtype=torch.int32)
+    lens = torch.randint(0, 17, (B,), generator=gen, device="cuda", dtype=torch.int32)
+    q = torch.randn((B, 2, 128), generator=gen, device="cuda").half()
+    kv = psa.KvCache(k, v, table, lens, 2)
+    out, lse = psa.window_attention(kv, q, 9, 2)
+    assert psa.read_device_error(out._workspace) == 0
+    for part in (slice(0, 60), slice(B - 60, B)):
+        some = psa.KvCache(k, v, table[part], lens[part], 2)
+        wr.close(out[part], lse[part], *reference(some, q[part], lens[part].tolist(), 9, 2))
+    table[8765] = 50
+    lens[8765] = 5
+    assert psa.read_device_error(psa.window_attention(kv, q, 9, 2, workspace=out._workspace)[0]._workspace) == 1
+    table[8765] = 0
+    lens[17] = 99
+    assert psa.read_device_error(psa.window_attention(kv, q, 9, 2, workspace=out._workspace)[0]._workspace) == 2
+    lens[17] = 3
+    assert psa.read_device_error(psa.window_attention(kv, q, 9, 2, workspace=out._workspace)[0]._workspace) == 0
