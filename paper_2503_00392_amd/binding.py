@@ -436,18 +436,21 @@ def _launch(call, at: int, stream, *args) -> int:
         raise ValueError(f"the stream is of {stream.device}, the tensors are on cuda:{at}")
     else:
         handle = stream.cuda_stream
-    if torch.cuda.current_device() == at:
+    if torch._C._cuda_getDevice() == at:
         return call(*args, handle)
     with torch.cuda.device(at):
         return call(*args, handle)
 
 
+def _refuse(name: str, t: torch.Tensor, what: str):
+    raise ValueError(f"{name}: {what} is wanted, not {t.dtype} {tuple(t.shape)} on {t.device} with strides {t.stride()}")
+
+
 def _tensor(name: str, t: torch.Tensor, shape: tuple, dtype, at: int) -> int:
     """The address of a contiguous tensor of just this shape, type and device."""
-    if t.shape != shape or t.dtype is not dtype or t.get_device() != at or not t.is_contiguous():
-        raise ValueError(f"{name}: a contiguous {dtype} tensor of shape {tuple(shape)} on device {at} is wanted, not {t.dtype} "
-                         f"{tuple(t.shape)} on {t.device} with strides {t.stride()}")
-    return t.data_ptr()
+    if t.shape == shape and t.dtype is dtype and t.get_device() == at and t.is_contiguous():
+        return t.data_ptr()
+    _refuse(name, t, f"a contiguous {dtype} tensor of shape {tuple(shape)} on device {at}")
 
 
 def _results(q: torch.Tensor, workspace, nbytes, out, lse, at: int, stream):
@@ -564,14 +567,13 @@ def packed_attention(cache: PackedCache, q: torch.Tensor, window: int = EVERYTHI
     return out, lse
 
 
-def _rows(name: str, t: torch.Tensor, tokens: int, dtype, at: int) -> int:
+def _rows(name: str, t: torch.Tensor, shape: tuple, dtype, at: int) -> int:
     """A [tokens][heads][128] tensor whose tokens may lie any distance apart: that distance in elements."""
-    shape, stride = t.shape, t.stride()
-    if len(shape) != 3 or shape[0] != tokens or shape[2] != 128 or t.dtype is not dtype or t.get_device() != at \
-            or (shape[1] > 1 and stride[1] != 128) or (shape[1] > 0 and stride[2] != 1):
-        raise ValueError(f"{name}: [{tokens}][heads][128] of {dtype} on device {at} with contiguous heads is wanted, not {t.dtype} "
-                         f"{tuple(shape)} on {t.device} with strides {stride}")
-    return stride[0] if tokens > 1 else 128 * shape[1]
+    if t.shape == shape and t.dtype is dtype and t.get_device() == at:
+        apart, head, channel = t.stride()
+        if (head == 128 or shape[1] < 2) and (channel == 1 or not shape[1]):
+            return apart if shape[0] > 1 else 128 * shape[1]
+    _refuse(name, t, f"{list(shape)} of {dtype} on device {at} with contiguous heads")
 
 
 def norm_rotate(q: torch.Tensor, k: torch.Tensor, positions: torch.Tensor, inv_freq: torch.Tensor, *,
@@ -579,21 +581,21 @@ def norm_rotate(q: torch.Tensor, k: torch.Tensor, positions: torch.Tensor, inv_f
                 interleaved: bool = False, q_out: torch.Tensor | None = None, k_out: torch.Tensor | None = None, stream=None):
     """psa_norm_rotate on q [T][Hq][128] and k [T][Hkv][128] (views of one projection's output will do); rotates the
     first 2 * len(inv_freq) channels; returns (q_out, k_out), which may be q and k themselves."""
-    T, dtype, at = q.shape[0], q.dtype, _device_of(q)
+    dtype, at = q.dtype, _device_of(q)
+    if q.dim() != 3 or k.dim() != 3:
+        raise ValueError("q and k are [tokens][heads][128]")
+    T, Hq, _ = q.shape
+    q_shape, k_shape, half = (T, Hq, 128), (T, k.shape[1], 128), inv_freq.numel()
     made = []
     if q_out is None:
-        made.append(q_out := torch.empty(q.shape, dtype=dtype, device=q.device))
+        made.append(q_out := torch.empty(q_shape, dtype=dtype, device=q.device))
     if k_out is None:
-        made.append(k_out := torch.empty(k.shape, dtype=dtype, device=q.device))
-    if q_out.shape != q.shape or k_out.shape != k.shape:
-        raise ValueError("q_out and k_out have the shapes of q and k")
-    if stream is not None:
+        made.append(k_out := torch.empty(k_shape, dtype=dtype, device=q.device))
+    if made and stream is not None:
         for t in made:
             t.record_stream(stream)
-    half = inv_freq.numel()
-    d = _RotateDesc(T, q.shape[1], k.shape[1], 128, 2 * half, bool(interleaved), bool(normalize), _dtype_code(dtype),
-                    _rows("q", q, T, dtype, at), _rows("k", k, T, dtype, at), _rows("q_out", q_out, T, dtype, at),
-                    _rows("k_out", k_out, T, dtype, at), eps)
+    d = _RotateDesc(T, Hq, k_shape[1], 128, 2 * half, bool(interleaved), bool(normalize), _dtype_code(dtype), _rows("q", q, q_shape, dtype, at),
+                    _rows("k", k, k_shape, dtype, at), _rows("q_out", q_out, q_shape, dtype, at), _rows("k_out", k_out, k_shape, dtype, at), eps)
     _check(_launch(load_library().psa_norm_rotate, at, stream, d, q.data_ptr(), k.data_ptr(), q_out.data_ptr(), k_out.data_ptr(),
                    None if q_weight is None or not normalize else _tensor("q_weight", q_weight, (128,), dtype, at),
                    None if k_weight is None or not normalize else _tensor("k_weight", k_weight, (128,), dtype, at),

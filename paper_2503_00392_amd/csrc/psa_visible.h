@@ -235,6 +235,7 @@ VisibleWs visible_ws(const psa_kv_desc *d, void *ws);
 hipError_t launch_clear(int32_t *header, hipStream_t st);
 hipError_t launch_join(const KvView &kv, const VisiblePlan &plan, const VisibleWs &ws, float *out, float *lse, hipStream_t st);
 
+__device__ __forceinline__ int clamp_ctx(const KvView &kv, int ctx) { return min(max(ctx, 0), kv.max_blocks * kPage); }
 __device__ __forceinline__ int visible_count(const KvView &kv, const VisiblePlan &plan, int r) {
     return make_visible(ctx_clamped_quiet(kv, r), plan.window, plan.num_sinks).count;
 }
@@ -247,11 +248,12 @@ __device__ __forceinline__ uint32_t pieces_of(uint32_t count, uint32_t length) {
 
 struct Piece {
     int r, b0, b1;                 // r = batch: there is no such piece
+    int length;                    // the request's, as given
     bool whole;                    // all of its request
 };
-__device__ __forceinline__ Piece make_piece(int r, uint32_t at, uint32_t count, uint32_t n) {
+__device__ __forceinline__ Piece make_piece(int r, int length, uint32_t at, uint32_t count, uint32_t n) {
     const uint32_t per = (count + n - 1) / n;
-    return {r, (int)(at * per), (int)min(count, (at + 1) * per), n == 1};
+    return {r, (int)(at * per), (int)min(count, (at + 1) * per), length, n == 1};
 }
 // Length of a piece; the last one of a request is a quarter of a piece too short in the mean: that much is left for it.
 __device__ __forceinline__ uint32_t piece_length(const KvView &kv, const VisiblePlan &plan, uint32_t total) {
@@ -268,15 +270,16 @@ __device__ __forceinline__ Piece find_piece(const KvView &kv, const VisiblePlan 
                                             PieceShared &sh) {
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     if (kv.batch <= 64) {                                // every wave by itself, a lane for each request
-        const uint32_t count = lane < kv.batch ? (uint32_t)visible_count(kv, plan, lane) : 0u;
+        const int given = lane < kv.batch ? kv.ctx_lens[lane] : 0;
+        const uint32_t count = (uint32_t)make_visible(clamp_ctx(kv, given), plan.window, plan.num_sinks).count;
         const uint32_t length = piece_length(kv, plan, (uint32_t)__builtin_amdgcn_readlane((int)wave_prefix_sum(count), 63));
         const uint32_t n = pieces_of(count, length), first = wave_prefix_sum(n) - n;
         if (leave && lane < kv.batch) ws.first[lane] = first;
         if (leave) ws.header[lane] = lane == 2 ? (int32_t)length : 0;
         const unsigned long long hit = __ballot(u >= first && u < first + n);
-        if (!hit) return {kv.batch, 0, 0, false};
+        if (!hit) return {kv.batch, 0, 0, 0, false};
         const int r = __builtin_ctzll(hit);
-        return make_piece(r, u - (uint32_t)__builtin_amdgcn_readlane((int)first, r), (uint32_t)__builtin_amdgcn_readlane((int)count, r),
+        return make_piece(r, __builtin_amdgcn_readlane(given, r), u - (uint32_t)__builtin_amdgcn_readlane((int)first, r), (uint32_t)__builtin_amdgcn_readlane((int)count, r),
                           (uint32_t)__builtin_amdgcn_readlane((int)n, r));
     }
     const uint32_t mine = tid < kv.batch ? (uint32_t)visible_count(kv, plan, tid) : 0u;
@@ -311,9 +314,9 @@ __device__ __forceinline__ Piece find_piece(const KvView &kv, const VisiblePlan 
     if (leave && tid < 64) ws.header[tid] = tid == 2 ? (int32_t)length : 0;
     __syncthreads();
     const int r = __builtin_amdgcn_readfirstlane(sh.r);
-    if (r >= kv.batch) return {r, 0, 0, false};
+    if (r >= kv.batch) return {r, 0, 0, 0, false};
     const uint32_t count = (uint32_t)__builtin_amdgcn_readfirstlane((int)sh.count);
-    return make_piece(r, (uint32_t)__builtin_amdgcn_readfirstlane((int)sh.at), count, pieces_of(count, length));
+    return make_piece(r, kv.ctx_lens[r], (uint32_t)__builtin_amdgcn_readfirstlane((int)sh.at), count, pieces_of(count, length));
 }
 
 }  // namespace psa

@@ -25,14 +25,16 @@ __global__ __launch_bounds__(256, 3) void window_kernel(KvView kv, const uint8_t
         return;
     }
     const int h = wg % kv.num_kv_heads, u = wg / kv.num_kv_heads;       // all of request u, or piece u
-    Piece piece{u, 0, 0, true};
-    if (!plan.direct) {
+    Piece piece{u, 0, 0, 0, true};
+    if (plan.direct) {
+        piece.length = kv.ctx_lens[u];
+    } else {
         __shared__ PieceShared shared_piece;
         piece = find_piece(kv, plan, (uint32_t)u, wg == 0, ws, shared_piece);
         if (piece.r >= kv.batch) return;
     }
-    const int r = piece.r, raw_ctx = kv.ctx_lens[r], ctx = ctx_clamped_quiet(kv, r);
-    int err = raw_ctx != ctx ? PSA_DEVERR_CTX_RANGE : 0;
+    const int r = piece.r, ctx = clamp_ctx(kv, piece.length);
+    int err = ctx != piece.length ? PSA_DEVERR_CTX_RANGE : 0;
     const Visible vis = make_visible(ctx, plan.window, plan.num_sinks);
     const int b0 = piece.b0, b1 = plan.direct ? vis.count : piece.b1;
 
