@@ -223,14 +223,14 @@ class KvCache:
     staging: object = None     # a Tier.staging_buffer or None (with a tier only)
 
     def desc(self) -> _KvDesc:
-        P, H, T, D = self.k_pool.shape
-        assert self.k_pool.is_contiguous() and self.v_pool.is_contiguous()
-        assert self.block_table.is_contiguous() and self.block_table.dtype == torch.int32
-        assert self.ctx_lens.dtype == torch.int32
-        return _KvDesc(self.block_table.shape[0], self.num_q_heads, H, D, T, P,
-                       self.block_table.shape[1], _dtype_code(self.k_pool.dtype),
-                       _ptr(self.k_pool), _ptr(self.v_pool), _ptr(self.block_table),
-                       _ptr(self.ctx_lens), self._tier_ptr())
+        k, v, table, lens = self.k_pool, self.v_pool, self.block_table, self.ctx_lens
+        P, H, T, D = k.shape
+        B, MB = table.shape
+        assert k.is_contiguous() and v.is_contiguous()
+        assert table.is_contiguous() and table.dtype is torch.int32
+        assert lens.dtype is torch.int32
+        return _KvDesc(B, self.num_q_heads, H, D, T, P, MB, _dtype_code(k.dtype), k.data_ptr(), v.data_ptr(),
+                       table.data_ptr(), lens.data_ptr(), None if self.tier is None else self._tier_ptr())
 
     def _tier_ptr(self):
         if self.tier is None:

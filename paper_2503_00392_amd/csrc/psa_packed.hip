@@ -206,7 +206,7 @@ __global__ __launch_bounds__(256, 3) void packed_kernel(KvView kv, const uint8_t
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);     // (so that table entries and page addresses are scalars)
     int wg = blockIdx.x;
     if (plan.checked && wg-- == 0) {
-        check_tables(kv, plan.window, plan.num_sinks, plan.blocks, ws.header, &sums.err[0]);
+        check_tables(kv, plan.window, plan.num_sinks, plan.blocks, ws.header);
         return;
     }
     const int h = wg % kv.num_kv_heads, u = wg / kv.num_kv_heads;       // all of request u, or piece u
@@ -374,7 +374,7 @@ hipError_t launch_append_packed(const psa_kv_desc *d, void *packed, const void *
 }
 
 // (measured: see the comment at the kernel)
-constexpr int kPackedGroups = 768, kPackedLeastBlocks = 32, kPackedDirectBlocks = 128;
+constexpr int kPackedGroups = 768, kPackedLeastBlocks = 32, kPackedDirectBlocks = 320;
 static VisiblePlan packed_plan(const psa_kv_desc *d, int window, int num_sinks) {
     return visible_plan(d, window, num_sinks, kPackedGroups, kPackedLeastBlocks, kPackedDirectBlocks);
 }

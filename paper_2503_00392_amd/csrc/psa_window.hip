@@ -21,7 +21,7 @@ __global__ __launch_bounds__(256, 3) void window_kernel(KvView kv, const uint8_t
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);     // (so that what hangs on it is a scalar)
     int wg = blockIdx.x;
     if (plan.checked && wg-- == 0) {
-        check_tables(kv, plan.window, plan.num_sinks, plan.blocks, ws.header, &sums.err[0]);
+        check_tables(kv, plan.window, plan.num_sinks, plan.blocks, ws.header);
         return;
     }
     const int h = wg % kv.num_kv_heads, u = wg / kv.num_kv_heads;       // all of request u, or piece u
@@ -206,7 +206,7 @@ VisiblePlan visible_plan(const psa_kv_desc *d, int window, int num_sinks, int gr
     const long long blocks = head + tail < d->max_blocks_per_seq ? head + tail : d->max_blocks_per_seq, all = d->batch * blocks;
     VisiblePlan p{window, num_sinks, (int)blocks, 1, least, false, false};
     p.direct = blocks <= least || (2 * S >= groups && blocks <= direct_blocks) || all > INT32_MAX;
-    p.checked = p.direct && all <= kCheckedEntries * (H >= 4 ? 16 : 1);
+    p.checked = p.direct && (all <= kCheckedEntries || (H >= 4 && all <= INT32_MAX));
     if (!p.direct) {
         const long long most = (all + least - 1) / least, want = (groups + H - 1) / H;
         p.groups = (int)(want < most ? want : (most > 0 ? most : 1));
@@ -240,7 +240,7 @@ hipError_t launch_join(const KvView &kv, const VisiblePlan &plan, const VisibleW
 }
 
 // (measured: see the comment at the kernel)
-constexpr int kWindowGroups = 512, kWindowLeastBlocks = 4, kWindowDirectBlocks = 128;
+constexpr int kWindowGroups = 512, kWindowLeastBlocks = 4, kWindowDirectBlocks = 320;
 static VisiblePlan window_plan(const psa_kv_desc *d, int window, int num_sinks) {
     return visible_plan(d, window, num_sinks, kWindowGroups, kWindowLeastBlocks, kWindowDirectBlocks);
 }
