@@ -359,7 +359,7 @@ psa_status psa_packed_attention(const psa_kv_desc *desc, const void *packed_pool
  *                 same stride; otherwise buffers do not overlap.
  *   q_weight, k_weight  [head_dim] of desc->dtype, or NULL for ones; not looked at without desc->normalize
  *   positions     [num_tokens] int32 (for the next token of each request: its ctx_lens before the append)
- *   inv_freq      [rot_dim / 2] float32; may be NULL with rot_dim 0
+ *   inv_freq      [rot_dim / 2] float32; it and positions may be NULL with rot_dim 0
  * Either head count may be 0 (then its pointers may be NULL).  All but positions and inv_freq 16-byte aligned, strides multiples
  * of 8 and at least heads * head_dim (outputs) or of any sign and size (inputs).
  * Errors: PSA_ERR_INVALID_ARG, PSA_ERR_UNSUPPORTED (head_dim != 128, more than 65536 heads, another dtype), PSA_ERR_LAUNCH.

@@ -470,19 +470,39 @@ def _results(q: torch.Tensor, workspace, nbytes, out, lse, at: int, stream):
     return workspace, out, lse
 
 
+def _tokens(n: int) -> int:
+    """A number of tokens as the 32 bits of the call hold it: beyond them it means all (or, below zero, an error) just as well."""
+    return min(max(int(n), -1), EVERYTHING)
+
+
+def _cache_on(kv: KvCache, at: int) -> _KvDesc:
+    """The descriptor of a cache whose tensors are where the kernels look for them (with a tier the pools are host memory)."""
+    k, v, table, lens, tier = kv.k_pool, kv.v_pool, kv.block_table, kv.ctx_lens, kv.tier
+    shape, dtype = k.shape, k.dtype
+    B, width = table.shape
+    if v.shape == shape and v.dtype is dtype and table.dtype is torch.int32 and lens.dtype is torch.int32 and lens.shape == (B,) \
+            and table.get_device() == at and lens.get_device() == at and k.is_contiguous() and v.is_contiguous() \
+            and table.is_contiguous() and lens.is_contiguous() and (tier is not None or (k.get_device() == at and v.get_device() == at)):
+        P, H, T, D = shape
+        return _KvDesc(B, kv.num_q_heads, H, D, T, P, width, _dtype_code(dtype), k.data_ptr(), v.data_ptr(), table.data_ptr(),
+                       lens.data_ptr(), None if tier is None else kv._tier_ptr())
+    raise ValueError(f"cache: contiguous pools of one shape and type and int32 tables [{B}][...] and lengths [{B}] on device {at} are wanted")
+
+
 def window_workspace_bytes(kv: KvCache, window: int, num_sinks: int = 0) -> int:
     d = kv.desc()
-    return int(load_library().psa_window_workspace_bytes(C.byref(d), int(window), int(num_sinks)))
+    return int(load_library().psa_window_workspace_bytes(d, _tokens(window), _tokens(num_sinks)))
 
 
 def window_attention(kv: KvCache, q: torch.Tensor, window: int, num_sinks: int = 0, *, workspace: torch.Tensor | None = None,
                      out: torch.Tensor | None = None, lse: torch.Tensor | None = None, stream=None):
     """psa_window_attention; returns (out float32 [B][Hq][128], lse float32 [B][Hq])."""
-    d, at = kv.desc(), _device_of(q)
+    at = _device_of(q)
+    d = _cache_on(kv, at)
     shape = (d.batch, d.num_q_heads, 128)
     where = _tensor("q", q, shape, kv.k_pool.dtype, at)
     workspace, out, lse = _results(q, workspace, lambda: window_workspace_bytes(kv, window, num_sinks), out, lse, at, stream)
-    _check(_launch(load_library().psa_window_attention, at, stream, d, where, window, num_sinks, _tensor("out", out, shape, torch.float32, at),
+    _check(_launch(load_library().psa_window_attention, at, stream, d, where, _tokens(window), _tokens(num_sinks), _tensor("out", out, shape, torch.float32, at),
                    _tensor("lse", lse, shape[:2], torch.float32, at), workspace.data_ptr(), workspace.nbytes), "psa_window_attention")
     out._workspace = workspace
     return out, lse
@@ -516,13 +536,11 @@ def _pages(kv: KvCache, packed: torch.Tensor, page_fill, page_list):
     """The device, the descriptor of the 16-bit side, and the addresses of the packed pool and the lists."""
     P, H = kv.k_pool.shape[:2]
     at = _device_of(packed)
-    if kv.k_pool.get_device() != at or kv.v_pool.get_device() != at:
-        raise ValueError("both caches are on one device")
     where = _tensor("packed pool", packed, (P, H, PACKED_RECORD_BYTES), torch.uint8, at)
     fill = None if page_fill is None else _tensor("page_fill", page_fill, (P,), torch.int32, at)
     n = 0 if page_list is None else page_list.numel()
     listed = None if page_list is None else _tensor("page_list", page_list, (n,), torch.int32, at)
-    return at, kv.desc(), where, fill, listed, n
+    return at, _cache_on(kv, at), where, fill, listed, n
 
 
 def pack_pages(kv: KvCache, packed: torch.Tensor, page_fill=None, page_list=None, stream=None) -> torch.Tensor:
@@ -549,7 +567,7 @@ def append_kv_packed(cache: PackedCache, k_new: torch.Tensor, v_new: torch.Tenso
 
 
 def packed_workspace_bytes(cache: PackedCache, window: int = EVERYTHING, num_sinks: int = 0) -> int:
-    return int(load_library().psa_packed_workspace_bytes(C.byref(cache._desc), int(window), int(num_sinks)))
+    return int(load_library().psa_packed_workspace_bytes(cache._desc, _tokens(window), _tokens(num_sinks)))
 
 
 def packed_attention(cache: PackedCache, q: torch.Tensor, window: int = EVERYTHING, num_sinks: int = 0, *,
@@ -560,7 +578,7 @@ def packed_attention(cache: PackedCache, q: torch.Tensor, window: int = EVERYTHI
     shape = (d.batch, d.num_q_heads, 128)
     where = _tensor("q", q, shape, cache.dtype, at)
     workspace, out, lse = _results(q, workspace, lambda: packed_workspace_bytes(cache, window, num_sinks), out, lse, at, stream)
-    _check(_launch(load_library().psa_packed_attention, at, stream, d, cache.pool.data_ptr(), where, window, num_sinks,
+    _check(_launch(load_library().psa_packed_attention, at, stream, d, cache.pool.data_ptr(), where, _tokens(window), _tokens(num_sinks),
                    _tensor("out", out, shape, torch.float32, at), _tensor("lse", lse, shape[:2], torch.float32, at),
                    workspace.data_ptr(), workspace.nbytes), "psa_packed_attention")
     out._workspace = workspace

@@ -325,6 +325,7 @@ psa_status psa_window_attention(const psa_kv_desc *d, const void *q, int32_t win
     }
     if (d->batch == 0) return PSA_OK;
     if (!q || !out || !workspace || !aligned16(q) || !aligned16(workspace)) return PSA_ERR_INVALID_ARG;
+    if (!aligned16(d->k_pool) || !aligned16(d->v_pool)) return PSA_ERR_INVALID_ARG;
     if (workspace_bytes < psa::window_workspace_bytes(d, window, num_sinks)) return PSA_ERR_WORKSPACE_TOO_SMALL;
     hipError_t e = psa::launch_window(d, q, window, num_sinks, out, lse, workspace, (hipStream_t)stream);
     return e == hipSuccess ? PSA_OK : PSA_ERR_LAUNCH;

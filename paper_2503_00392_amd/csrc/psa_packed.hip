@@ -210,12 +210,11 @@ __global__ __launch_bounds__(256, 3) void packed_kernel(KvView kv, const uint8_t
         return;
     }
     const int h = wg % kv.num_kv_heads, u = wg / kv.num_kv_heads;       // all of request u, or piece u
-    Piece piece{u, 0, 0, 0, true};
+    Piece piece{u, 0, 0, 0, -1, true};
     if (plan.direct) {
         piece.length = kv.ctx_lens[u];
     } else {
-        __shared__ PieceShared shared_piece;
-        piece = find_piece(kv, plan, (uint32_t)u, wg == 0, ws, shared_piece);
+        piece = find_piece(kv, plan, (uint32_t)u, wg == 0, ws);
         if (piece.r >= kv.batch) return;
     }
     const int r = piece.r, ctx = clamp_ctx(kv, piece.length);
@@ -337,11 +336,12 @@ __global__ __launch_bounds__(256, 3) void packed_kernel(KvView kv, const uint8_t
     if (rg == 0 && hd < G && part == 0) { sums.m[wave][hd] = limit == -INFINITY ? -INFINITY : ref; sums.l[wave][hd] = l; }
     const bool bad_ctx = __ballot(err & PSA_DEVERR_CTX_RANGE) != 0ull, bad_page = __ballot(err & PSA_DEVERR_PAGE_RANGE) != 0ull;
     if (lane == 0) sums.err[wave] = (bad_ctx ? PSA_DEVERR_CTX_RANGE : 0) | (bad_page ? PSA_DEVERR_PAGE_RANGE : 0);
-    if (plan.direct && !plan.checked && sums.err[wave] && lane == 0) set_error(ws.header, sums.err[wave]);
+    // (where the header was cleared by a launch before; otherwise the checking workgroup or the joining launch sets the word)
+    if ((plan.listed || (plan.direct && !plan.checked)) && sums.err[wave] && lane == 0) set_error(ws.header, sums.err[wave]);
     __syncthreads();
     const size_t row = (size_t)r * kv.num_q_heads + h * G;
     join_waves<G>(sums, tid, piece.whole, out + row * kHeadDim, lse ? lse + row : nullptr,
-                  plan.direct ? nullptr : ws.records + (size_t)wg * G * kSplitStride);
+                  piece.record < 0 ? nullptr : ws.records + ((size_t)piece.record * kv.num_kv_heads + h) * G * kSplitStride);
 }
 
 // ---- host side ----------------------------------------------------------------------------------
@@ -388,6 +388,7 @@ static hipError_t launch_packed_t(const KvView &kv, const void *q, const Visible
                                   hipStream_t st) {
     const unsigned grid = (unsigned)(kv.num_kv_heads * (plan.direct ? kv.batch : plan.groups + kv.batch) + plan.checked);
     if (plan.direct && !plan.checked && launch_clear(ws.header, st) != hipSuccess) return hipErrorLaunchFailure;
+    if (plan.listed && launch_list(kv, plan, ws, st) != hipSuccess) return hipErrorLaunchFailure;
     packed_kernel<DT, G><<<grid, 256, 0, st>>>(kv, (const uint8_t *)q, plan, ws, out, lse);
     const hipError_t e = hipGetLastError();
     return e == hipSuccess && !plan.direct ? launch_join(kv, plan, ws, out, lse, st) : e;
@@ -406,7 +407,7 @@ hipError_t launch_packed(const psa_kv_desc *d, const void *packed, const void *q
     }
     const int G = d->num_q_heads / d->num_kv_heads;
     const VisiblePlan plan = packed_plan(d, window, num_sinks);
-    const VisibleWs vws = visible_ws(d, ws);
+    const VisibleWs vws = visible_ws(d, plan, ws);
 #define PSA_CASE(DT, GG) \
     if (d->dtype == DT && G == GG) return launch_packed_t<DT, GG>(kv, q, plan, vws, out, lse, st);
     PSA_CASE(0, 1) PSA_CASE(0, 2) PSA_CASE(0, 4) PSA_CASE(0, 8)

@@ -54,7 +54,7 @@ __global__ __launch_bounds__(256) void rotate_kernel(RotateArgs a) {
     float c[4], s[4];
     // byte offsets of the lane's two groups of four channels (PAIRED: eight neighbours, pairs interleaved)
     const int i0 = 4 * cl, lo = PAIRED ? 8 * cl : (i0 < a.half ? i0 : a.half + i0), hi = PAIRED ? 8 * cl + 4 : (i0 < a.half ? i0 + a.half : 64 + i0);
-    const double position = (double)a.positions[token];
+    const double position = a.half ? (double)a.positions[token] : 0.0;      // (without rotation there may be none)
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
         c[j] = 1.0f;

@@ -235,8 +235,9 @@ __device__ __forceinline__ void check_tables(const KvView &kv, int window, int n
 //            and none has much to read.
 //   planned  workgroups take pieces of requests: a piece is what the visible blocks of all requests come to, divided by the
 //            workgroups that fill the GPU, and a request gets as many as it takes -- one long request among short ones is
-//            shared by many.  A piece's result is a record, unless it is all of its request, and a second launch joins the records of a request.  Every workgroup finds
-//            its piece from the lengths by itself; the first one also leaves the requests' first records for the launch that joins.
+//            shared by many.  A piece's result is a record, unless it is all of its request, and a second launch joins the records of a request.  Up to
+//            kFoundRequests requests every workgroup finds its piece from the lengths by itself (a microsecond), the first one also leaves
+//            the requests' first records for the launch that joins; for more a launch before lists the pieces.
 // Few pieces, because what a workgroup does before its first block and after its last (dependent trips to memory, the
 // exchange between its waves) costs as much as twenty blocks: the same bytes in pieces of half the size and two
 // rounds of workgroups took 15 % longer.  So a request keeps one piece (or two, ...) up to a quarter more than these hold.
@@ -244,19 +245,23 @@ struct VisiblePlan {
     int window, num_sinks;
     int blocks;                    // visible blocks of a request at most
     int groups, least;             // planned: workgroups for a KV head that fill the GPU; blocks of a piece at least
-    bool direct, checked;          // checked: direct, and few enough table entries for check_tables
+    bool direct, checked, listed;  // checked: direct, and few enough table entries for check_tables; listed: planned, with a list
 };
 VisiblePlan visible_plan(const psa_kv_desc *d, int window, int num_sinks, int groups, int least, int direct_blocks);
 size_t visible_workspace_bytes(const psa_kv_desc *d, const VisiblePlan &p);
 
-// The workspace: header (word 1: error bits, word 2: length of a piece), the requests' first records, the records.
+constexpr int kFoundRequests = 64, kListedRequests = 65536;      // (beyond: direct)
+// The workspace: header (word 1: error bits, word 2: length of a piece, word 3: pieces in the list), the requests' first records,
+// the list (request, first and last block, record or -1 where the piece is all of the request), the records.
 struct VisibleWs {
     int32_t *header;
     uint32_t *first;               // [batch]
-    float *records;                // [groups + batch][num_kv_heads][G][kSplitStride]
+    int4 *list;                    // [groups + batch] if listed
+    float *records;                // [groups + batch][num_kv_heads][G][kSplitStride]; listed: [2 groups]..., for requests in several pieces
 };
-VisibleWs visible_ws(const psa_kv_desc *d, void *ws);
+VisibleWs visible_ws(const psa_kv_desc *d, const VisiblePlan &p, void *ws);
 hipError_t launch_clear(int32_t *header, hipStream_t st);
+hipError_t launch_list(const KvView &kv, const VisiblePlan &plan, const VisibleWs &ws, hipStream_t st);
 hipError_t launch_join(const KvView &kv, const VisiblePlan &plan, const VisibleWs &ws, float *out, float *lse, hipStream_t st);
 
 __device__ __forceinline__ int visible_count(const KvView &kv, const VisiblePlan &plan, int r) {
@@ -272,74 +277,34 @@ __device__ __forceinline__ uint32_t pieces_of(uint32_t count, uint32_t length) {
 struct Piece {
     int r, b0, b1;                 // r = batch: there is no such piece
     int length;                    // the request's, as given
+    int record;                    // -1: none
     bool whole;                    // all of its request
 };
-__device__ __forceinline__ Piece make_piece(int r, int length, uint32_t at, uint32_t count, uint32_t n) {
-    const uint32_t per = (count + n - 1) / n;
-    return {r, (int)(at * per), (int)min(count, (at + 1) * per), length, n == 1};
-}
 // Length of a piece; the last one of a request is a quarter of a piece too short in the mean: that much is left for it.
 __device__ __forceinline__ uint32_t piece_length(const KvView &kv, const VisiblePlan &plan, uint32_t total) {
-    const uint32_t share = max(plan.groups - kv.batch / 4, (plan.groups + 1) / 2);
+    const uint32_t share = (uint32_t)max(plan.groups - kv.batch / 4, (plan.groups + 1) / 2);
     return max((total + share - 1) / share, (uint32_t)plan.least);
 }
-struct PieceShared {
-    uint32_t wave[4];
-    int r;
-    uint32_t at, count;            // which of the request's pieces, and its blocks
-};
-// Piece u.  256 threads; `leave`: this workgroup leaves the requests' first records and the length of a piece.
-__device__ __forceinline__ Piece find_piece(const KvView &kv, const VisiblePlan &plan, uint32_t u, bool leave, const VisibleWs &ws,
-                                            PieceShared &sh) {
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    if (kv.batch <= 64) {                                // every wave by itself, a lane for each request
-        const int given = lane < kv.batch ? kv.ctx_lens[lane] : 0;
-        const uint32_t count = (uint32_t)make_visible(clamp_ctx(kv, given), plan.window, plan.num_sinks).count;
-        const uint32_t length = piece_length(kv, plan, (uint32_t)__builtin_amdgcn_readlane((int)wave_prefix_sum(count), 63));
-        const uint32_t n = pieces_of(count, length), first = wave_prefix_sum(n) - n;
-        if (leave && lane < kv.batch) ws.first[lane] = first;
-        if (leave) ws.header[lane] = lane == 2 ? (int32_t)length : 0;
-        const unsigned long long hit = __ballot(u >= first && u < first + n);
-        if (!hit) return {kv.batch, 0, 0, 0, false};
-        const int r = __builtin_ctzll(hit);
-        return make_piece(r, __builtin_amdgcn_readlane(given, r), u - (uint32_t)__builtin_amdgcn_readlane((int)first, r), (uint32_t)__builtin_amdgcn_readlane((int)count, r),
-                          (uint32_t)__builtin_amdgcn_readlane((int)n, r));
+// Piece u; `leave`: this workgroup leaves the requests' first records and the length of a piece.
+__device__ __forceinline__ Piece find_piece(const KvView &kv, const VisiblePlan &plan, uint32_t u, bool leave, const VisibleWs &ws) {
+    if (plan.listed) {
+        const int4 e = ws.list[u];
+        if (u >= (uint32_t)ws.header[3]) return {kv.batch, 0, 0, 0, -1, false};
+        return {e.x, e.y, e.z, kv.ctx_lens[e.x], e.w, e.w < 0};
     }
-    const uint32_t mine = tid < kv.batch ? (uint32_t)visible_count(kv, plan, tid) : 0u;
-    uint32_t sum = mine;
-    for (int r = tid + 256; r < kv.batch; r += 256) sum += (uint32_t)visible_count(kv, plan, r);
-    sum = wave_prefix_sum(sum);
-    if (lane == 63) sh.wave[wave] = sum;
-    if (tid == 0) sh.r = kv.batch;
-    __syncthreads();
-    const uint32_t length = piece_length(kv, plan, sh.wave[0] + sh.wave[1] + sh.wave[2] + sh.wave[3]);
-    uint32_t before = 0;
-    for (int r0 = 0; r0 < kv.batch; r0 += 256) {
-        const int r = r0 + tid;
-        const uint32_t count = r0 == 0 ? mine : (r < kv.batch ? (uint32_t)visible_count(kv, plan, r) : 0u);
-        const uint32_t n = pieces_of(count, length), upto = wave_prefix_sum(n);
-        __syncthreads();                                 // (the sums of the step before have been read)
-        if (lane == 63) sh.wave[wave] = upto;
-        __syncthreads();
-        uint32_t first = before + upto - n;
-#pragma unroll
-        for (int w = 0; w < 4; ++w) {
-            if (w < wave) first += sh.wave[w];
-            before += sh.wave[w];
-        }
-        if (leave && r < kv.batch) ws.first[r] = first;
-        if (u >= first && u < first + n) {
-            sh.r = r;
-            sh.at = u - first;
-            sh.count = count;
-        }
-    }
-    if (leave && tid < 64) ws.header[tid] = tid == 2 ? (int32_t)length : 0;
-    __syncthreads();
-    const int r = __builtin_amdgcn_readfirstlane(sh.r);
-    if (r >= kv.batch) return {r, 0, 0, 0, false};
-    const uint32_t count = (uint32_t)__builtin_amdgcn_readfirstlane((int)sh.count);
-    return make_piece(r, kv.ctx_lens[r], (uint32_t)__builtin_amdgcn_readfirstlane((int)sh.at), count, pieces_of(count, length));
+    const int lane = threadIdx.x & 63;                   // every wave by itself, a lane for each request
+    const int given = lane < kv.batch ? kv.ctx_lens[lane] : 0;
+    const uint32_t count = (uint32_t)make_visible(clamp_ctx(kv, given), plan.window, plan.num_sinks).count;
+    const uint32_t length = piece_length(kv, plan, (uint32_t)__builtin_amdgcn_readlane((int)wave_prefix_sum(count), 63));
+    const uint32_t n = pieces_of(count, length), first = wave_prefix_sum(n) - n;
+    if (leave && lane < kv.batch) ws.first[lane] = first;
+    if (leave) ws.header[lane] = lane == 2 ? (int32_t)length : 0;
+    const unsigned long long hit = __ballot(u >= first && u < first + n);
+    if (!hit) return {kv.batch, 0, 0, 0, -1, false};
+    const int r = __builtin_ctzll(hit);
+    const uint32_t at = u - (uint32_t)__builtin_amdgcn_readlane((int)first, r), all = (uint32_t)__builtin_amdgcn_readlane((int)count, r),
+                   of = (uint32_t)__builtin_amdgcn_readlane((int)n, r), per = (all + of - 1) / of;
+    return {r, (int)(at * per), (int)min(all, (at + 1) * per), __builtin_amdgcn_readlane(given, r), (int)u, of == 1};
 }
 
 }  // namespace psa

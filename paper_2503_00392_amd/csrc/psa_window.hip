@@ -25,12 +25,11 @@ __global__ __launch_bounds__(256, 3) void window_kernel(KvView kv, const uint8_t
         return;
     }
     const int h = wg % kv.num_kv_heads, u = wg / kv.num_kv_heads;       // all of request u, or piece u
-    Piece piece{u, 0, 0, 0, true};
+    Piece piece{u, 0, 0, 0, -1, true};
     if (plan.direct) {
         piece.length = kv.ctx_lens[u];
     } else {
-        __shared__ PieceShared shared_piece;
-        piece = find_piece(kv, plan, (uint32_t)u, wg == 0, ws, shared_piece);
+        piece = find_piece(kv, plan, (uint32_t)u, wg == 0, ws);
         if (piece.r >= kv.batch) return;
     }
     const int r = piece.r, ctx = clamp_ctx(kv, piece.length);
@@ -110,11 +109,12 @@ __global__ __launch_bounds__(256, 3) void window_kernel(KvView kv, const uint8_t
     if (rg == 0 && hd < G && part == 0) { sums.m[wave][hd] = limit == -INFINITY ? -INFINITY : ref; sums.l[wave][hd] = l; }
     const bool bad_ctx = __ballot(err & PSA_DEVERR_CTX_RANGE) != 0ull, bad_page = __ballot(err & PSA_DEVERR_PAGE_RANGE) != 0ull;
     if (lane == 0) sums.err[wave] = (bad_ctx ? PSA_DEVERR_CTX_RANGE : 0) | (bad_page ? PSA_DEVERR_PAGE_RANGE : 0);
-    if (plan.direct && !plan.checked && sums.err[wave] && lane == 0) set_error(ws.header, sums.err[wave]);
+    // (where the header was cleared by a launch before; otherwise the checking workgroup or the joining launch sets the word)
+    if ((plan.listed || (plan.direct && !plan.checked)) && sums.err[wave] && lane == 0) set_error(ws.header, sums.err[wave]);
     __syncthreads();
     const size_t row = (size_t)r * kv.num_q_heads + h * G;
     join_waves<G>(sums, tid, piece.whole, out + row * kHeadDim, lse ? lse + row : nullptr,
-                  plan.direct ? nullptr : ws.records + (size_t)wg * G * kSplitStride);
+                  piece.record < 0 ? nullptr : ws.records + ((size_t)piece.record * kv.num_kv_heads + h) * G * kSplitStride);
 }
 
 // grid (batch * num_q_heads); LANES record lanes x 32 quarters of a row.  Lane j takes the request's records j, j + LANES, ... in
@@ -146,6 +146,7 @@ __global__ __launch_bounds__(32 * LANES) void join_kernel(KvView kv, VisiblePlan
     if (n > 1) load(sl);
     float M = -INFINITY;
     int err = ctx != kv.ctx_lens[r] ? PSA_DEVERR_CTX_RANGE : 0;
+    if (n == 1 && plan.listed) return;                   // (there is no record, and the word is set)
     for (uint32_t i = tid; i < n; i += 32 * LANES) {
         M = fmaxf(M, src[i * stride]);
         if (g == 0) err |= __float_as_int(src[i * stride + 2]);
@@ -198,36 +199,86 @@ __global__ __launch_bounds__(32 * LANES) void join_kernel(KvView kv, VisiblePlan
 
 __global__ void clear_error_word_kernel(int32_t *header) { header[threadIdx.x] = 0; }
 
+// The list of pieces of more than kFoundRequests requests, by one workgroup: the sum of the visible blocks, then, 1024 requests at a
+// time, how many pieces come before each.
+__global__ __launch_bounds__(1024) void list_kernel(KvView kv, VisiblePlan plan, VisibleWs ws) {
+    __shared__ uint32_t part[2][16];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    uint32_t sum = 0;
+    for (int r = tid; r < kv.batch; r += 1024) sum += (uint32_t)visible_count(kv, plan, r);
+    sum = wave_prefix_sum(sum);
+    if (lane == 63) part[0][wave] = sum;
+    __syncthreads();
+    uint32_t total = 0, pieces = 0, records = 0;         // the latter two: before the requests at hand
+    for (int w = 0; w < 16; ++w) total += part[0][w];
+    const uint32_t length = piece_length(kv, plan, total);
+    for (int r0 = 0; r0 < kv.batch; r0 += 1024) {
+        const int r = r0 + tid;
+        const uint32_t count = r < kv.batch ? (uint32_t)visible_count(kv, plan, r) : 0u;
+        const uint32_t n = pieces_of(count, length), several = n > 1 ? n : 0u;
+        const uint32_t upto = wave_prefix_sum(n), upto_several = wave_prefix_sum(several);
+        __syncthreads();                                 // (what the step before left has been read)
+        if (lane == 63) { part[0][wave] = upto; part[1][wave] = upto_several; }
+        __syncthreads();
+        uint32_t at = pieces + upto - n, record = records + upto_several - several;
+        for (int w = 0; w < 16; ++w) {
+            if (w < wave) { at += part[0][w]; record += part[1][w]; }
+            pieces += part[0][w];
+            records += part[1][w];
+        }
+        if (r < kv.batch) ws.first[r] = record;
+        if (n) {
+            const uint32_t per = (count + n - 1) / n;
+            for (uint32_t i = 0; i < n; ++i)
+                ws.list[at + i] = make_int4(r, (int)(i * per), (int)min(count, (i + 1) * per), n > 1 ? (int)(record + i) : -1);
+        }
+    }
+    if (tid < 64) ws.header[tid] = tid == 2 ? (int32_t)length : (tid == 3 ? (int32_t)pieces : 0);
+}
+
 // ---- host side ----------------------------------------------------------------------------------
 VisiblePlan visible_plan(const psa_kv_desc *d, int window, int num_sinks, int groups, int least, int direct_blocks) {
     const long long H = d->num_kv_heads, S = d->batch * H;
     // a window of w tokens lies in at most (w + 14) / 16 + 1 blocks
     const long long tail = window > 0 ? ((long long)window + 14) / kPage + 1 : 0, head = ((long long)num_sinks + kPage - 1) / kPage;
     const long long blocks = head + tail < d->max_blocks_per_seq ? head + tail : d->max_blocks_per_seq, all = d->batch * blocks;
-    VisiblePlan p{window, num_sinks, (int)blocks, 1, least, false, false};
-    p.direct = blocks <= least || (2 * S >= groups && blocks <= direct_blocks) || all > INT32_MAX;
+    VisiblePlan p{window, num_sinks, (int)blocks, 1, least, false, false, false};
+    p.direct = blocks <= least || (2 * S >= groups && blocks <= direct_blocks) || all > INT32_MAX || d->batch > kListedRequests;
     p.checked = p.direct && (all <= kCheckedEntries || (H >= 4 && all <= INT32_MAX));
     if (!p.direct) {
         const long long most = (all + least - 1) / least, want = (groups + H - 1) / H;
         p.groups = (int)(want < most ? want : (most > 0 ? most : 1));
+        p.listed = d->batch > kFoundRequests;
     }
     return p;
 }
 
 static size_t first_bytes(const psa_kv_desc *d) { return ((size_t)d->batch * 4 + 255) / 256 * 256; }
+static size_t list_bytes(const psa_kv_desc *d, const VisiblePlan &p) {
+    return p.listed ? ((size_t)(p.groups + d->batch) * sizeof(int4) + 255) / 256 * 256 : 0;
+}
 
 size_t visible_workspace_bytes(const psa_kv_desc *d, const VisiblePlan &p) {
     if (p.direct) return 256;
-    return 256 + first_bytes(d) + (size_t)(d->batch + p.groups) * d->num_q_heads * kSplitStride * sizeof(float);
+    // A request in n > 1 pieces of length L has more than 5/4 L blocks, and n < blocks / L + 1 < 9/5 blocks / L: listed, all those
+    // together have fewer than twice as many records as there are groups.
+    const size_t records = p.listed ? 2 * (size_t)p.groups : (size_t)d->batch + p.groups;
+    return 256 + first_bytes(d) + list_bytes(d, p) + records * d->num_q_heads * kSplitStride * sizeof(float);
 }
 
-VisibleWs visible_ws(const psa_kv_desc *d, void *ws) {
-    uint8_t *base = static_cast<uint8_t *>(ws);
-    return {reinterpret_cast<int32_t *>(base), reinterpret_cast<uint32_t *>(base + 256), reinterpret_cast<float *>(base + 256 + first_bytes(d))};
+VisibleWs visible_ws(const psa_kv_desc *d, const VisiblePlan &p, void *ws) {
+    uint8_t *base = static_cast<uint8_t *>(ws), *list = base + 256 + first_bytes(d);
+    return {reinterpret_cast<int32_t *>(base), reinterpret_cast<uint32_t *>(base + 256), reinterpret_cast<int4 *>(list),
+            reinterpret_cast<float *>(list + list_bytes(d, p))};
 }
 
 hipError_t launch_clear(int32_t *header, hipStream_t st) {
     clear_error_word_kernel<<<1, 64, 0, st>>>(header);
+    return hipGetLastError();
+}
+
+hipError_t launch_list(const KvView &kv, const VisiblePlan &plan, const VisibleWs &ws, hipStream_t st) {
+    list_kernel<<<1, 1024, 0, st>>>(kv, plan, ws);
     return hipGetLastError();
 }
 
@@ -254,6 +305,7 @@ static hipError_t launch_window_t(const KvView &kv, const void *q, const Visible
                                   hipStream_t st) {
     const unsigned grid = (unsigned)(kv.num_kv_heads * (plan.direct ? kv.batch : plan.groups + kv.batch) + plan.checked);
     if (plan.direct && !plan.checked && launch_clear(ws.header, st) != hipSuccess) return hipErrorLaunchFailure;
+    if (plan.listed && launch_list(kv, plan, ws, st) != hipSuccess) return hipErrorLaunchFailure;
     window_kernel<DT, G><<<grid, 256, 0, st>>>(kv, (const uint8_t *)q, plan, ws, out, lse);
     const hipError_t e = hipGetLastError();
     return e == hipSuccess && !plan.direct ? launch_join(kv, plan, ws, out, lse, st) : e;
@@ -270,7 +322,7 @@ hipError_t launch_window(const psa_kv_desc *d, const void *q, int window, int nu
     }
     const int G = d->num_q_heads / d->num_kv_heads;
     const VisiblePlan plan = window_plan(d, window, num_sinks);
-    const VisibleWs vws = visible_ws(d, ws);
+    const VisibleWs vws = visible_ws(d, plan, ws);
 #define PSA_CASE(DT, GG) \
     if (d->dtype == DT && G == GG) return launch_window_t<DT, GG>(kv, q, plan, vws, out, lse, st);
     PSA_CASE(0, 1) PSA_CASE(0, 2) PSA_CASE(0, 4) PSA_CASE(0, 8)

@@ -112,3 +112,16 @@ def test_extremes(psa):
     assert not normed[0, 0].any() and torch.isnan(normed[0, 4]).all()
     rows = [1, 2, 5]
     check(normed[:, rows], *reference(x[:, rows], None, pos, freq, 1e-30, True, False))
+
+
+def test_norm_alone_needs_no_positions(psa):
+    """At the C boundary: without rotation the positions and frequencies may be NULL."""
+    import ctypes as C
+    from paper_2503_00392_amd import binding as pb
+    x = torch.randn((3, 5, 128), device="cuda").half()
+    y = torch.zeros_like(x)
+    d = pb._RotateDesc(3, 5, 0, 128, 0, 0, 1, 0, 640, 0, 640, 0, 1e-6)
+    assert psa.load_library().psa_norm_rotate(C.byref(d), x.data_ptr(), None, y.data_ptr(), None, None, None, None, None, None) == 0
+    torch.cuda.synchronize()
+    none = torch.empty(0, device="cuda")
+    check(y, *reference(x, None, torch.zeros(3), none, 1e-6, True, False))

@@ -188,7 +188,7 @@ def test_host_tier(psa):
     assert torch.equal(want[0], got[0]) and torch.equal(want[1], got[1])
 
 
-@pytest.mark.parametrize("B,H,G", [(5, 8, 4), (64, 2, 8), (65, 1, 1), (70, 5, 2), (256, 1, 4), (257, 3, 8), (600, 1, 4)])
+@pytest.mark.parametrize("B,H,G", [(5, 8, 4), (64, 2, 8), (65, 1, 1), (70, 5, 2), (256, 1, 4), (257, 3, 8), (600, 1, 4), (1030, 1, 2)])
 def test_one_long_request_among_short_ones(psa, B, H, G):
     """Pieces: a long request is cut into many, the others are one each, some requests are empty; batches about the sizes where a
     workgroup finds its piece in another way."""

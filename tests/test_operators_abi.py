@@ -57,7 +57,7 @@ def test_attention_refuses_bad_descriptors(lib, kw, want):
 @pytest.mark.parametrize("call", [_window, _packed])
 def test_attention_refuses_bad_arguments(lib, call):
     d = _desc()
-    for kw in (dict(window=-1), dict(sinks=-1), dict(q=None), dict(out=None), dict(ws=None), dict(q=0x108)):
+    for kw in (dict(window=-1), dict(sinks=-1), dict(q=None), dict(out=None), dict(ws=None), dict(q=0x108), dict(ws=0x308)):
         assert call(lib, d, **kw) == INVALID, kw
     assert call(lib, d, ws_bytes=255) == SMALL
     assert call(lib, _desc(batch=0, block_table=None, ctx_lens=None), q=None, out=None, ws=None) == OK
@@ -81,6 +81,16 @@ def test_workspaces_follow_what_can_be_visible(lib):
         everything = size(C.byref(long), psa.EVERYTHING, psa.EVERYTHING)
         assert 256 <= size(C.byref(long), 64, 4) < size(C.byref(long), 16384, 4) <= everything < 1 << 28
         assert size(C.byref(_desc(batch=0, max_blocks_per_seq=0, block_table=None, ctx_lens=None)), 9, 9) >= 256
+
+
+def test_windows_beyond_32_bits_keep_their_meaning(lib):
+    """The binding hands 32 bits on: what is larger means everything, what is below zero is refused."""
+    kv = psa.KvCache(*(torch.zeros((8, 2, 16, 128)).half() for _ in range(2)), torch.zeros((1, 4000), dtype=torch.int32),
+                     torch.zeros(1, dtype=torch.int32), 8)
+    packed = psa.PackedCache(psa.PackedCache.empty_pool(8, 2, device="cpu"), kv.block_table, kv.ctx_lens, 8, torch.float16)
+    for size, cache in ((psa.window_workspace_bytes, kv), (psa.packed_workspace_bytes, packed)):
+        assert size(cache, 1 << 40, 0) == size(cache, 0, 1 << 32) == size(cache, psa.EVERYTHING, 0) > size(cache, 1024, 0)
+        assert size(cache, -(1 << 40), 0) == 0 and size(cache, 5, -1) == 0
 
 
 def test_page_calls_refuse(lib):
@@ -163,6 +173,12 @@ def test_binding_refuses_before_it_calls():
                  lambda: psa.norm_rotate(q[:, :, ::2], q, lens, torch.ones(64))):
         with pytest.raises(ValueError):
             call()
+    pools = [torch.zeros((8, 2, 16, 128), dtype=torch.bfloat16) for _ in range(2)]
+    for bad in (psa.KvCache(pools[0], pools[1][:4], table, lens, 8), psa.KvCache(pools[0], pools[1].half(), table, lens, 8),
+                psa.KvCache(*pools, table, lens[:1], 8), psa.KvCache(*pools, table, torch.zeros((2, 2), dtype=torch.int32)[:, 0], 8),
+                psa.KvCache(*pools, table.long(), lens, 8), psa.KvCache(pools[0].transpose(0, 1), pools[1].transpose(0, 1), table, lens, 8)):
+        with pytest.raises(ValueError):
+            pb._cache_on(bad, -1)
     with pytest.raises(TypeError):
         psa.PackedCache(pool, table, lens, 8, torch.float32)
 
