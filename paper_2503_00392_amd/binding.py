@@ -528,9 +528,6 @@ class PackedCache:
     def empty_pool(num_pages: int, num_kv_heads: int, device="cuda") -> torch.Tensor:
         return torch.zeros((num_pages, num_kv_heads, PACKED_RECORD_BYTES), dtype=torch.uint8, device=device)
 
-    def desc(self) -> _KvDesc:
-        return self._desc
-
 
 def _pages(kv: KvCache, packed: torch.Tensor, page_fill, page_list):
     """The device, the descriptor of the 16-bit side, and the addresses of the packed pool and the lists."""

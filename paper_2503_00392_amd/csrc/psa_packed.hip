@@ -86,7 +86,8 @@ __device__ __forceinline__ int value_offset(int t, int cl) { return kPackedV + (
 
 // ---- pages --------------------------------------------------------------------------------------
 // Bound by memory: 8192 bytes in and 2176 out for a (listed page, KV head), one wave each; lane (rg, cl) takes rows 4 i + rg,
-// channels 8 cl .. + 7, so loads are whole kilobytes and the stores of one instruction lie in 256 bytes.
+// channels 8 cl .. + 7, so loads are whole kilobytes and the stores of one instruction lie in 256 bytes.  8192 pages of 8 KV heads:
+// 117 us = 5.8 TB/s, and 121 us back (a large copy: 4.9); 64 of them 3.5 us each way.
 template <int DT>
 __global__ __launch_bounds__(256) void pack_kernel(const uint8_t *__restrict__ k_pool, const uint8_t *__restrict__ v_pool,
                                                    uint8_t *__restrict__ packed, const int32_t *__restrict__ page_fill,
@@ -191,12 +192,20 @@ __device__ __forceinline__ PackedPage load_packed(const uint8_t *rec, uint32_t l
 }
 __device__ __forceinline__ uint32_t word_of(const uint4 &v, int w) { return w == 0 ? v.x : (w == 1 ? v.y : (w == 2 ? v.z : v.w)); }
 
-// grid: one workgroup of four waves per split and (request, KV head), before them the one that checks the tables (if any).  A wave takes pairs of visible blocks.
+// grid: one workgroup of four waves per piece (or request) and KV head, before them the one that checks the tables (if any).
+// A wave takes pairs of visible blocks.
 //   logits  D[token][row] = K[token][channel] Q[channel][row], four 16x16x32 products a block: elements and power become
 //           bfloat16, exactly.  A query in bfloat16 stands in all rows of its head; one in binary16 is split into two
 //           bfloat16 parts in neighbouring rows (8 + 3 bits, exact), whose sums are added.
 //   values  D[row][channel] += P[row][token] V[token][channel], one 16x16x32 product for eight channels of the pair's 32
 //           tokens.  Lane (rg, cl) has the logits of tokens 4 rg .. + 3 of both pages and loads just those tokens' values.
+// (The matrix cores also take 4-bit elements and their powers as they are, with 8-bit floating parts of the query, but then
+// add 128 products of different sizes with an error of 1e-5 of the sum of these sizes in the mean; these sums leave 1e-7.)
+// Bound by memory: 4 requests of 128K tokens, 8 KV heads: 93 us = 6.1 TB/s at G = 4 (the call, with the launch that joins, 100),
+// vector ALUs 46 % busy -- 64 conversions, 36 permutations and some 100 others for a pair of blocks --, matrix cores 12 %.  What brought
+// it there from 173 us: the next pair under way (140), weight parts by masks and not by branches (127), table entries from
+// a list that is loaded 64 blocks ahead and not each before its page (103).  Three pairs under way take as long; a workgroup needs
+// two others on its CU (768 in all).
 template <int DT, int G>
 __global__ __launch_bounds__(256, 3) void packed_kernel(KvView kv, const uint8_t *__restrict__ q, VisiblePlan plan,
                                                         VisibleWs ws, float *__restrict__ out, float *__restrict__ lse) {
@@ -307,8 +316,10 @@ __global__ __launch_bounds__(256, 3) void packed_kernel(KvView kv, const uint8_t
 #pragma unroll
             for (int j = 0; j < 8; ++j)
                 x[j] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(word_of(pg[j >> 2].v, j & 3), power[j], u));
-            const uint4 even = make_uint4(pick_halves<false>(x[0], x[1]), pick_halves<false>(x[2], x[3]), pick_halves<false>(x[4], x[5]), pick_halves<false>(x[6], x[7]));
-            const uint4 odd = make_uint4(pick_halves<true>(x[0], x[1]), pick_halves<true>(x[2], x[3]), pick_halves<true>(x[4], x[5]), pick_halves<true>(x[6], x[7]));
+            const uint4 even = make_uint4(pick_halves<false>(x[0], x[1]), pick_halves<false>(x[2], x[3]),
+                                          pick_halves<false>(x[4], x[5]), pick_halves<false>(x[6], x[7]));
+            const uint4 odd = make_uint4(pick_halves<true>(x[0], x[1]), pick_halves<true>(x[2], x[3]),
+                                         pick_halves<true>(x[4], x[5]), pick_halves<true>(x[6], x[7]));
 #pragma unroll
             for (int y = 0; y < kProducts<1, G>; ++y) {
                 acc[2 * u] = mfma_16x16x32<1>(a[y], even, acc[2 * u]);
@@ -373,7 +384,8 @@ hipError_t launch_append_packed(const psa_kv_desc *d, void *packed, const void *
     return hipGetLastError();
 }
 
-// (measured: see the comment at the kernel)
+// 768 workgroups: see the kernel.  Pieces of 32 blocks at least: one request of 32K tokens takes 14.4 us, 16.5 with 16, 16.2 with 48.  One
+// launch up to 320 blocks: 64 requests with windows of 2040 tokens 28 us (39 in pieces), of 4000 49 (57), of 8000 77 (69).
 constexpr int kPackedGroups = 768, kPackedLeastBlocks = 32, kPackedDirectBlocks = 320;
 static VisiblePlan packed_plan(const psa_kv_desc *d, int window, int num_sinks) {
     return visible_plan(d, window, num_sinks, kPackedGroups, kPackedLeastBlocks, kPackedDirectBlocks);

@@ -1,16 +1,22 @@
 // Decode attention over the paged 16-bit cache with a sliding window and a few first tokens that stay visible (sinks):
-// softmax(q k / sqrt d) v over the tokens t < sinks and t >= ctx - window, with one pass over them, and the launch that
-// joins the splits of a request (also those of the 4-bit cache).
+// softmax(q k / sqrt d) v over the tokens t < sinks and t >= ctx - window, with one pass over them; and what it shares with the
+// 4-bit cache's attention: how a call is cut, the list of pieces, the launch that joins the pieces of a request.
 #include "psa_fold.h"
 #include "psa_host.h"
 #include "psa_visible.h"
 
 namespace psa {
 
-// grid: one workgroup of four waves per split and (request, KV head), before them the one that checks the tables (if any).  A wave takes every fourth of the split's visible blocks and carries its own online softmax over them, as
-// the dense control does (see there): logits with four 16x16x32 products, lane (kq, n) = (lane / 16, lane % 16) getting the
-// logits of the head of row n for tokens kq, 4+kq, 8+kq, 12+kq; values with eight 16x16x16 products, the weights in parts in
-// a head's rows.  Tokens of a block that the query does not see get the logit -inf and a zero value row (the page may hold NaN there).
+// grid: one workgroup of four waves per piece (or request) and KV head, before them the one that checks the tables (if any).
+// A wave takes every fourth visible block and carries its own online softmax over them: logits with four 16x16x32 products,
+// lane (kq, n) = (lane / 16, lane % 16) getting the logits of the head of row n for tokens kq, 4+kq, 8+kq, 12+kq; values with eight
+// 16x16x16 products, the weights in parts in a head's rows.  Tokens of a block that the query does not see get the logit -inf and a
+// zero value row (the page may hold NaN there).
+// Bound by memory: 4 requests of 64K tokens, 8 KV heads, G = 4: 165 us a call = 6.5 TB/s; 64 ragged requests with a window of 4096
+// and 16 sinks, G = 8: 160 us = 6.4; 240 ragged ones with a window of 130, 4 KV heads: 17 us = 3.8, of which 5 are the way to the first
+// block and from the last.  Keys and values are both loaded a block ahead: with the values loaded when their block's turn came
+// the second took 178 us at the best number of workgroups.  Two workgroups on a CU are enough and more get in each
+// other's way: 155 us with 512 of them, 184 to 188 with 1024 to 2048 (limited to two on a CU by LDS: 175 to 184).
 template <int DT, int G>
 __global__ __launch_bounds__(256, 3) void window_kernel(KvView kv, const uint8_t *__restrict__ q, VisiblePlan plan,
                                                         VisibleWs ws, float *__restrict__ out, float *__restrict__ lse) {
@@ -290,7 +296,8 @@ hipError_t launch_join(const KvView &kv, const VisiblePlan &plan, const VisibleW
     return hipGetLastError();
 }
 
-// (measured: see the comment at the kernel)
+// 512 workgroups: see the kernel.  One launch up to 320 blocks (windows of 5K): ragged and equal batches of 32 to 128 requests with
+// windows of 4000 tokens took 79 to 365 us that way, 90 to 381 in pieces; with windows of 8000 it is 122 against 113 and 168 against 189.
 constexpr int kWindowGroups = 512, kWindowLeastBlocks = 4, kWindowDirectBlocks = 320;
 static VisiblePlan window_plan(const psa_kv_desc *d, int window, int num_sinks) {
     return visible_plan(d, window, num_sinks, kWindowGroups, kWindowLeastBlocks, kWindowDirectBlocks);
