@@ -419,6 +419,8 @@ def dense_attention(kv: KvCache, q: torch.Tensor, *, workspace: torch.Tensor | N
 # ---- window and sinks, the 4-bit cache, norm and rotation --------------------------------------------------------------
 PACKED_RECORD_BYTES = 2176
 EVERYTHING = 2 ** 31 - 1      # a window that holds every token
+_current_device = getattr(torch._C, "_cuda_getDevice", None)                  # (None in a torch without a GPU: no call gets there)
+_raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
 
 def _device_of(t: torch.Tensor) -> int:
@@ -428,18 +430,21 @@ def _device_of(t: torch.Tensor) -> int:
     return at
 
 
-def _launch(call, at: int, stream, *args) -> int:
+def _launch(call, at: int, stream, *args) -> None:
     """call(*args, stream) with the tensors' device as the current one, on the caller's stream or that device's current one."""
     if stream is None:
-        handle = torch._C._cuda_getCurrentRawStream(at)
+        handle = _raw_stream(at)
     elif stream.device.index != at:
         raise ValueError(f"the stream is of {stream.device}, the tensors are on cuda:{at}")
     else:
         handle = stream.cuda_stream
-    if torch._C._cuda_getDevice() == at:
-        return call(*args, handle)
-    with torch.cuda.device(at):
-        return call(*args, handle)
+    if _current_device() == at:
+        status = call(*args, handle)
+    else:
+        with torch.cuda.device(at):
+            status = call(*args, handle)
+    if status != PSA_OK:
+        raise PsaError(status, call.__name__)
 
 
 def _refuse(name: str, t: torch.Tensor, what: str):
@@ -453,13 +458,11 @@ def _tensor(name: str, t: torch.Tensor, shape: tuple, dtype, at: int) -> int:
     _refuse(name, t, f"a contiguous {dtype} tensor of shape {tuple(shape)} on device {at}")
 
 
-def _results(q: torch.Tensor, workspace, nbytes, out, lse, at: int, stream):
-    """The caller's buffers, or new ones (not given back to the allocator before `stream` is done with them)."""
+def _results(q: torch.Tensor, workspace, nbytes, out, lse, stream):
+    """The caller's buffers, and new ones where there are none (not given back to the allocator before `stream` is done with them)."""
     made = []
     if workspace is None:
-        made.append(workspace := torch.empty(nbytes(), dtype=torch.uint8, device=q.device))
-    elif workspace.get_device() != at or not workspace.is_contiguous():
-        raise ValueError("workspace: a contiguous tensor on the device of q is wanted")
+        made.append(workspace := torch.empty(nbytes, dtype=torch.uint8, device=q.device))
     if out is None:
         made.append(out := torch.empty(q.shape, dtype=torch.float32, device=q.device))
     if lse is None:
@@ -470,9 +473,16 @@ def _results(q: torch.Tensor, workspace, nbytes, out, lse, at: int, stream):
     return workspace, out, lse
 
 
+def _scratch(workspace: torch.Tensor, at: int) -> int:
+    if workspace.get_device() == at and workspace.is_contiguous():
+        return workspace.data_ptr()
+    _refuse("workspace", workspace, f"a contiguous tensor on device {at}")
+
+
 def _tokens(n: int) -> int:
     """A number of tokens as the 32 bits of the call hold it: beyond them it means all (or, below zero, an error) just as well."""
-    return min(max(int(n), -1), EVERYTHING)
+    n = int(n)
+    return n if -1 <= n <= EVERYTHING else (EVERYTHING if n > 0 else -1)
 
 
 def _cache_on(kv: KvCache, at: int) -> _KvDesc:
@@ -499,11 +509,12 @@ def window_attention(kv: KvCache, q: torch.Tensor, window: int, num_sinks: int =
     """psa_window_attention; returns (out float32 [B][Hq][128], lse float32 [B][Hq])."""
     at = _device_of(q)
     d = _cache_on(kv, at)
-    shape = (d.batch, d.num_q_heads, 128)
+    shape, window, num_sinks = (d.batch, d.num_q_heads, 128), _tokens(window), _tokens(num_sinks)
     where = _tensor("q", q, shape, kv.k_pool.dtype, at)
-    workspace, out, lse = _results(q, workspace, lambda: window_workspace_bytes(kv, window, num_sinks), out, lse, at, stream)
-    _check(_launch(load_library().psa_window_attention, at, stream, d, where, _tokens(window), _tokens(num_sinks), _tensor("out", out, shape, torch.float32, at),
-                   _tensor("lse", lse, shape[:2], torch.float32, at), workspace.data_ptr(), workspace.nbytes), "psa_window_attention")
+    if workspace is None or out is None or lse is None:
+        workspace, out, lse = _results(q, workspace, 0 if workspace is not None else window_workspace_bytes(kv, window, num_sinks), out, lse, stream)
+    _launch(load_library().psa_window_attention, at, stream, d, where, window, num_sinks, _tensor("out", out, shape, torch.float32, at),
+            _tensor("lse", lse, shape[:2], torch.float32, at), _scratch(workspace, at), workspace.nbytes)
     out._workspace = workspace
     return out, lse
 
@@ -523,6 +534,7 @@ class PackedCache:
         self.num_q_heads, self.num_kv_heads, self.dtype = int(num_q_heads), int(pool.shape[1]), dtype
         self._desc = _KvDesc(block_table.shape[0], self.num_q_heads, self.num_kv_heads, 128, 16, pool.shape[0],
                              block_table.shape[1], _dtype_code(dtype), None, None, _ptr(block_table), _ptr(ctx_lens), None)
+        self._q_shape, self._kv_shape = ((block_table.shape[0], n, 128) for n in (self.num_q_heads, self.num_kv_heads))
 
     @staticmethod
     def empty_pool(num_pages: int, num_kv_heads: int, device="cuda") -> torch.Tensor:
@@ -543,24 +555,22 @@ def _pages(kv: KvCache, packed: torch.Tensor, page_fill, page_list):
 def pack_pages(kv: KvCache, packed: torch.Tensor, page_fill=None, page_list=None, stream=None) -> torch.Tensor:
     """psa_pack_pages: pages of `kv` to records of the packed pool, in place; returns the pool."""
     at, d, where, fill, listed, n = _pages(kv, packed, page_fill, page_list)
-    _check(_launch(load_library().psa_pack_pages, at, stream, d, where, fill, listed, n), "psa_pack_pages")
+    _launch(load_library().psa_pack_pages, at, stream, d, where, fill, listed, n)
     return packed
 
 
 def unpack_pages(kv: KvCache, packed: torch.Tensor, page_list=None, stream=None) -> None:
     """psa_unpack_pages: records of the packed pool to pages of `kv`, whose pools it writes."""
     at, d, where, _, listed, n = _pages(kv, packed, None, page_list)
-    _check(_launch(load_library().psa_unpack_pages, at, stream, d, where, listed, n), "psa_unpack_pages")
+    _launch(load_library().psa_unpack_pages, at, stream, d, where, listed, n)
 
 
 def append_kv_packed(cache: PackedCache, k_new: torch.Tensor, v_new: torch.Tensor, status: torch.Tensor | None = None,
                      stream=None) -> None:
     """psa_append_kv_packed: writes into cache.pool and cache.ctx_lens in place."""
-    d, at = cache._desc, _device_of(cache.pool)
-    shape = (d.batch, d.num_kv_heads, 128)
-    _check(_launch(load_library().psa_append_kv_packed, at, stream, d, cache.pool.data_ptr(), _tensor("k_new", k_new, shape, cache.dtype, at),
-                   _tensor("v_new", v_new, shape, cache.dtype, at),
-                   None if status is None else _tensor("status", status, (d.batch,), torch.int32, at)), "psa_append_kv_packed")
+    at, shape = _device_of(cache.pool), cache._kv_shape
+    _launch(load_library().psa_append_kv_packed, at, stream, cache._desc, cache.pool.data_ptr(), _tensor("k_new", k_new, shape, cache.dtype, at),
+            _tensor("v_new", v_new, shape, cache.dtype, at), None if status is None else _tensor("status", status, shape[:1], torch.int32, at))
 
 
 def packed_workspace_bytes(cache: PackedCache, window: int = EVERYTHING, num_sinks: int = 0) -> int:
@@ -571,13 +581,12 @@ def packed_attention(cache: PackedCache, q: torch.Tensor, window: int = EVERYTHI
                      workspace: torch.Tensor | None = None, out: torch.Tensor | None = None, lse: torch.Tensor | None = None,
                      stream=None):
     """psa_packed_attention; returns (out float32 [B][Hq][128], lse float32 [B][Hq])."""
-    d, at = cache._desc, _device_of(cache.pool)
-    shape = (d.batch, d.num_q_heads, 128)
+    at, shape, window, num_sinks = _device_of(cache.pool), cache._q_shape, _tokens(window), _tokens(num_sinks)
     where = _tensor("q", q, shape, cache.dtype, at)
-    workspace, out, lse = _results(q, workspace, lambda: packed_workspace_bytes(cache, window, num_sinks), out, lse, at, stream)
-    _check(_launch(load_library().psa_packed_attention, at, stream, d, cache.pool.data_ptr(), where, _tokens(window), _tokens(num_sinks),
-                   _tensor("out", out, shape, torch.float32, at), _tensor("lse", lse, shape[:2], torch.float32, at),
-                   workspace.data_ptr(), workspace.nbytes), "psa_packed_attention")
+    if workspace is None or out is None or lse is None:
+        workspace, out, lse = _results(q, workspace, 0 if workspace is not None else packed_workspace_bytes(cache, window, num_sinks), out, lse, stream)
+    _launch(load_library().psa_packed_attention, at, stream, cache._desc, cache.pool.data_ptr(), where, window, num_sinks,
+            _tensor("out", out, shape, torch.float32, at), _tensor("lse", lse, shape[:2], torch.float32, at), _scratch(workspace, at), workspace.nbytes)
     out._workspace = workspace
     return out, lse
 
@@ -601,21 +610,23 @@ def norm_rotate(q: torch.Tensor, k: torch.Tensor, positions: torch.Tensor, inv_f
         raise ValueError("q and k are [tokens][heads][128]")
     T, Hq, _ = q.shape
     q_shape, k_shape, half = (T, Hq, 128), (T, k.shape[1], 128), inv_freq.numel()
-    made = []
-    if q_out is None:
-        made.append(q_out := torch.empty(q_shape, dtype=dtype, device=q.device))
-    if k_out is None:
-        made.append(k_out := torch.empty(k_shape, dtype=dtype, device=q.device))
-    if made and stream is not None:
-        for t in made:
-            t.record_stream(stream)
+    if q_out is None or k_out is None:
+        made = []
+        if q_out is None:
+            made.append(q_out := torch.empty(q_shape, dtype=dtype, device=q.device))
+        if k_out is None:
+            made.append(k_out := torch.empty(k_shape, dtype=dtype, device=q.device))
+        if stream is not None:
+            for t in made:
+                t.record_stream(stream)
+    if not normalize:
+        q_weight = k_weight = None
     d = _RotateDesc(T, Hq, k_shape[1], 128, 2 * half, bool(interleaved), bool(normalize), _dtype_code(dtype), _rows("q", q, q_shape, dtype, at),
                     _rows("k", k, k_shape, dtype, at), _rows("q_out", q_out, q_shape, dtype, at), _rows("k_out", k_out, k_shape, dtype, at), eps)
-    _check(_launch(load_library().psa_norm_rotate, at, stream, d, q.data_ptr(), k.data_ptr(), q_out.data_ptr(), k_out.data_ptr(),
-                   None if q_weight is None or not normalize else _tensor("q_weight", q_weight, (128,), dtype, at),
-                   None if k_weight is None or not normalize else _tensor("k_weight", k_weight, (128,), dtype, at),
-                   _tensor("positions", positions, (T,), torch.int32, at), _tensor("inv_freq", inv_freq, (half,), torch.float32, at)),
-           "psa_norm_rotate")
+    _launch(load_library().psa_norm_rotate, at, stream, d, q.data_ptr(), k.data_ptr(), q_out.data_ptr(), k_out.data_ptr(),
+            None if q_weight is None else _tensor("q_weight", q_weight, (128,), dtype, at),
+            None if k_weight is None else _tensor("k_weight", k_weight, (128,), dtype, at),
+            _tensor("positions", positions, (T,), torch.int32, at), _tensor("inv_freq", inv_freq, (half,), torch.float32, at))
     return q_out, k_out
 
 
