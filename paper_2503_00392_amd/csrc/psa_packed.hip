@@ -385,10 +385,12 @@ hipError_t launch_append_packed(const psa_kv_desc *d, void *packed, const void *
 }
 
 // 768 workgroups: see the kernel.  Pieces of 32 blocks at least: one request of 32K tokens takes 14.4 us, 16.5 with 16, 16.2 with 48.  One
-// launch up to 320 blocks: 64 requests with windows of 2040 tokens 28 us (39 in pieces), of 4000 49 (57), of 8000 77 (69).
-constexpr int kPackedGroups = 768, kPackedLeastBlocks = 32, kPackedDirectBlocks = 320;
+// launch up to 320 blocks from 192 (request, KV head) pairs on: 64 requests of 8 KV heads with windows of 2040 tokens 28 us (39 in
+// pieces), of 4000 49 (57), of 8000 77 (69); 32 requests of 1024 tokens 11.4 (14.9), of 4096 30.7 (33.4); 16 requests of 1024 9.6 (11.9),
+// of 2048 15.4 (15.3), of 4096 26.8 (22.3).
+constexpr int kPackedGroups = 768, kPackedLeastBlocks = 32, kPackedDirectFrom = 192;
 static VisiblePlan packed_plan(const psa_kv_desc *d, int window, int num_sinks) {
-    return visible_plan(d, window, num_sinks, kPackedGroups, kPackedLeastBlocks, kPackedDirectBlocks);
+    return visible_plan(d, window, num_sinks, kPackedGroups, kPackedLeastBlocks, kPackedDirectFrom);
 }
 
 size_t packed_workspace_bytes(const psa_kv_desc *d, int window, int num_sinks) {

@@ -231,8 +231,8 @@ __device__ __forceinline__ void check_tables(const KvView &kv, int window, int n
 }
 
 // How a call is cut.
-//   direct   a workgroup for every (request, KV head), which writes the results: where there are enough of them to fill the GPU
-//            and none has much to read.
+//   direct   a workgroup for every (request, KV head), which writes the results: where none has more than kDirectBlocks to read
+//            and there are direct_from of them, or, as the second launch costs 3 to 4 us, where they are fewer and have little to read.
 //   planned  workgroups take pieces of requests: a piece is what the visible blocks of all requests come to, divided by the
 //            workgroups that fill the GPU, and a request gets as many as it takes -- one long request among short ones is
 //            shared by many.  A piece's result is a record, unless it is all of its request, and a second launch joins
@@ -250,9 +250,10 @@ struct VisiblePlan {
     int groups, least;             // planned: workgroups for a KV head that fill the GPU; blocks of a piece at least
     bool direct, checked, listed;  // checked: direct, and few enough table entries for check_tables; listed: planned, with a list
 };
-VisiblePlan visible_plan(const psa_kv_desc *d, int window, int num_sinks, int groups, int least, int direct_blocks);
+VisiblePlan visible_plan(const psa_kv_desc *d, int window, int num_sinks, int groups, int least, int direct_from);
 size_t visible_workspace_bytes(const psa_kv_desc *d, const VisiblePlan &p);
 
+constexpr int kDirectBlocks = 320;
 constexpr int kFoundRequests = 64, kListedRequests = 65536;      // (beyond: direct)
 // The workspace: header (word 1: error bits, word 2: length of a piece, word 3: pieces in the list), the requests' first records,
 // the list (request, first and last block, record or -1 where the piece is all of the request), the records.

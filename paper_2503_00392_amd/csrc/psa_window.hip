@@ -243,13 +243,13 @@ __global__ __launch_bounds__(1024) void list_kernel(KvView kv, VisiblePlan plan,
 }
 
 // ---- host side ----------------------------------------------------------------------------------
-VisiblePlan visible_plan(const psa_kv_desc *d, int window, int num_sinks, int groups, int least, int direct_blocks) {
+VisiblePlan visible_plan(const psa_kv_desc *d, int window, int num_sinks, int groups, int least, int direct_from) {
     const long long H = d->num_kv_heads, S = d->batch * H;
     // a window of w tokens lies in at most (w + 14) / 16 + 1 blocks
     const long long tail = window > 0 ? ((long long)window + 14) / kPage + 1 : 0, head = ((long long)num_sinks + kPage - 1) / kPage;
     const long long blocks = head + tail < d->max_blocks_per_seq ? head + tail : d->max_blocks_per_seq, all = d->batch * blocks;
     VisiblePlan p{window, num_sinks, (int)blocks, 1, least, false, false, false};
-    p.direct = blocks <= least || (2 * S >= groups && blocks <= direct_blocks) || all > INT32_MAX || d->batch > kListedRequests;
+    p.direct = blocks <= least || blocks <= (S >= direct_from ? kDirectBlocks : S / 2) || all > INT32_MAX || d->batch > kListedRequests;
     p.checked = p.direct && (all <= kCheckedEntries || (H >= 4 && all <= INT32_MAX));
     if (!p.direct) {
         const long long most = (all + least - 1) / least, want = (groups + H - 1) / H;
@@ -296,11 +296,13 @@ hipError_t launch_join(const KvView &kv, const VisiblePlan &plan, const VisibleW
     return hipGetLastError();
 }
 
-// 512 workgroups: see the kernel.  One launch up to 320 blocks (windows of 5K): ragged and equal batches of 32 to 128 requests with
-// windows of 4000 tokens took 79 to 365 us that way, 90 to 381 in pieces; with windows of 8000 it is 122 against 113 and 168 against 189.
-constexpr int kWindowGroups = 512, kWindowLeastBlocks = 4, kWindowDirectBlocks = 320;
+// 512 workgroups: see the kernel.  One launch up to 320 blocks (windows of 5K) from 256 (request, KV head) pairs on: ragged and equal
+// batches of 32 to 128 requests and 8 KV heads with windows of 4000 tokens took 79 to 365 us that way, 90 to 381 in pieces; with
+// windows of 8000 it is 122 against 113 and 168 against 189.  16 requests: of 1024 tokens 16.3 against 18.0, of 2048 29.4 against 28.0, of
+// 4096 61 against 49; 8 requests: of 600 10.5 against 11.0, of 1024 15.0 against 13.0.
+constexpr int kWindowGroups = 512, kWindowLeastBlocks = 4, kWindowDirectFrom = 256;
 static VisiblePlan window_plan(const psa_kv_desc *d, int window, int num_sinks) {
-    return visible_plan(d, window, num_sinks, kWindowGroups, kWindowLeastBlocks, kWindowDirectBlocks);
+    return visible_plan(d, window, num_sinks, kWindowGroups, kWindowLeastBlocks, kWindowDirectFrom);
 }
 
 size_t window_workspace_bytes(const psa_kv_desc *d, int window, int num_sinks) {
