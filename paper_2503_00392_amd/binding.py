@@ -542,14 +542,20 @@ class PackedCache:
 
 
 def _pages(kv: KvCache, packed: torch.Tensor, page_fill, page_list):
-    """The device, the descriptor of the 16-bit side, and the addresses of the packed pool and the lists."""
-    P, H = kv.k_pool.shape[:2]
-    at = _device_of(packed)
+    """The device, the descriptor of the 16-bit side (without its tables, which play no part), and the addresses of the packed
+    pool and the lists."""
+    at, k, v = _device_of(packed), kv.k_pool, kv.v_pool
+    shape, dtype = k.shape, k.dtype
+    if not (v.shape == shape and v.dtype is dtype and k.get_device() == at and v.get_device() == at and k.is_contiguous() and v.is_contiguous()
+            and kv.tier is None):
+        raise ValueError(f"cache: contiguous pools of one shape and type on device {at}, without a tier, are wanted")
+    P, H, T, D = shape
     where = _tensor("packed pool", packed, (P, H, PACKED_RECORD_BYTES), torch.uint8, at)
     fill = None if page_fill is None else _tensor("page_fill", page_fill, (P,), torch.int32, at)
     n = 0 if page_list is None else page_list.numel()
     listed = None if page_list is None else _tensor("page_list", page_list, (n,), torch.int32, at)
-    return at, _cache_on(kv, at), where, fill, listed, n
+    d = _KvDesc(0, kv.num_q_heads, H, D, T, P, 0, _dtype_code(dtype), k.data_ptr(), v.data_ptr(), None, None, None)
+    return at, d, where, fill, listed, n
 
 
 def pack_pages(kv: KvCache, packed: torch.Tensor, page_fill=None, page_list=None, stream=None) -> torch.Tensor:
