@@ -50,11 +50,12 @@ template <int DT, bool PAIRED>
 __global__ __launch_bounds__(256) void rotate_kernel(RotateArgs a) {
     const int lane = threadIdx.x & 63, rg = lane >> 4, cl = lane & 15;
     const long long wave = (long long)blockIdx.x * 4 + (threadIdx.x >> 6);
-    const int token = (int)(wave / a.waves_per_token), first = (int)(wave % a.waves_per_token) * a.rows_per_wave;
+    const long long token = wave / a.waves_per_token;
     if (token >= a.tokens) return;
+    const int first = (int)(wave % a.waves_per_token) * a.rows_per_wave;
     const int rows = a.q_heads + a.kv_heads, last = min(rows, first + a.rows_per_wave);
     float c[4], s[4];
-    // byte offsets of the lane's two groups of four channels (PAIRED: eight neighbours, pairs interleaved)
+    // first channels of the lane's two groups of four (PAIRED: eight neighbours, pairs interleaved)
     const int i0 = 4 * cl, lo = PAIRED ? 8 * cl : (i0 < a.half ? i0 : a.half + i0), hi = PAIRED ? 8 * cl + 4 : (i0 < a.half ? i0 + a.half : 64 + i0);
     const double position = a.half ? (double)a.positions[token] : 0.0;      // (without rotation there may be none)
 #pragma unroll

@@ -210,6 +210,21 @@ def test_one_long_request_among_short_ones(psa, B, H, G):
     assert psa.read_device_error(out._workspace) == 3
 
 
+def test_so_many_requests_that_no_pieces_are_listed(psa):
+    B, width = 66000, 40
+    gen = torch.Generator(device="cuda").manual_seed(4)
+    k, v = (torch.randn((64, 1, 16, 128), generator=gen, device="cuda").bfloat16() for _ in range(2))
+    table = torch.randint(0, 64, (B, width), generator=gen, device="cuda", dtype=torch.int32)
+    lens = torch.randint(0, 40, (B,), generator=gen, device="cuda", dtype=torch.int32)
+    lens[-3:] = torch.tensor([640, 0, 333])
+    q = torch.randn((B, 1, 128), generator=gen, device="cuda").bfloat16()
+    out, lse = psa.window_attention(psa.KvCache(k, v, table, lens, 1), q, INT_MAX)
+    assert psa.read_device_error(out._workspace) == 0
+    for part in (slice(0, 50), slice(B - 50, B)):
+        some = psa.KvCache(k, v, table[part], lens[part], 1)
+        wr.close(out[part], lse[part], *reference(some, q[part], lens[part].tolist(), INT_MAX, 0))
+
+
 def test_so_many_requests_that_no_workgroup_checks_the_tables(psa):
     B = 9000
     gen = torch.Generator(device="cuda").manual_seed(3)
