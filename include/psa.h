@@ -302,14 +302,15 @@ psa_status psa_dense_attention(const psa_kv_desc *desc, const void *q, float *ou
  *                      alone, both 0 nothing
  *   out  [batch][num_q_heads][head_dim] float32; lse [batch][num_q_heads] float32 natural-log sum of exponentiated scaled
  *        logits, may be NULL.  Where nothing is visible out = 0 and lse = -inf; a NaN in a visible key or value shows in the
- *        outputs of its heads
+ *        outputs of its heads, an infinity in a visible value gives infinities or NaN
  *   workspace  psa_window_workspace_bytes of the same descriptor, window and num_sinks; holds the sticky error word
  * A call repeated gives the same bits.  How a request is cut, and with it the order of its sums, follows from the lengths of all
  * requests of the batch: its results can differ in the last bits from those it has in another batch.
  * Pages without a visible token are not looked at, nor are their block-table entries: they may have been freed.  What a
  * page holds beside the visible tokens does not matter (NaN included).
- * Shapes as for psa_dense_attention, max_blocks_per_seq up to 2^27 - 1; q and workspace 16-byte aligned.  With a second tier slices are read
- * from where the pools are.
+ * Shapes as for psa_dense_attention, max_blocks_per_seq up to 2^27 - 1, batch * num_kv_heads up to 2^23, batch * num_q_heads
+ * up to 2^24 (PSA_ERR_UNSUPPORTED beyond, also for psa_append_kv_packed and psa_packed_attention); q and workspace 16-byte
+ * aligned.  With a second tier slices are read from where the pools are.
  */
 size_t psa_window_workspace_bytes(const psa_kv_desc *desc, int32_t window, int32_t num_sinks);
 psa_status psa_window_attention(const psa_kv_desc *desc, const void *q, int32_t window, int32_t num_sinks, float *out, float *lse,
@@ -328,7 +329,8 @@ psa_status psa_window_attention(const psa_kv_desc *desc, const void *q, int32_t 
  * psa_unpack_pages only and may be NULL elsewhere.  A descriptor with a second tier is PSA_ERR_UNSUPPORTED.
  *
  * psa_pack_pages: pages of the 16-bit cache to records.  page_fill, page_list, num_listed as for psa_build_block_metadata;
- *   tokens beyond a page's fill are written as zeros and not looked at.
+ *   tokens beyond a page's fill are written as zeros and not looked at.  A call takes up to 2^25 pages times KV heads
+ *   (beyond: PSA_ERR_UNSUPPORTED), psa_unpack_pages also.
  * psa_unpack_pages: records to pages of the 16-bit cache (WRITES desc->k_pool and desc->v_pool), rounded to desc->dtype: exact in
  *   bfloat16.  page_list, num_listed as above.
  * psa_append_kv_packed: as psa_append_kv, with the token going to the packed pool, bit for bit as psa_pack_pages packs
@@ -362,7 +364,7 @@ psa_status psa_packed_attention(const psa_kv_desc *desc, const void *packed_pool
  *   inv_freq      [rot_dim / 2] float32; it and positions may be NULL with rot_dim 0
  * Either head count may be 0 (then its pointers may be NULL).  All but positions and inv_freq 16-byte aligned, strides multiples
  * of 8 and at least heads * head_dim (outputs) or of any sign and size (inputs).
- * Errors: PSA_ERR_INVALID_ARG, PSA_ERR_UNSUPPORTED (head_dim != 128, more than 65536 heads, another dtype), PSA_ERR_LAUNCH.
+ * Errors: PSA_ERR_INVALID_ARG, PSA_ERR_UNSUPPORTED (head_dim != 128, more than 65536 heads or 2^25 tokens, another dtype), PSA_ERR_LAUNCH.
  */
 typedef struct {
     int32_t num_tokens;

@@ -279,9 +279,10 @@ namespace {
 
 bool aligned16(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
 
-// Lengths stay below 2^31 tokens.
+// Lengths stay below 2^31 tokens, launches below 2^32 threads: 256 for a request and KV head, 128 for a head's join.
 psa_status check_window(const psa_kv_desc *d, int32_t window, int32_t num_sinks) {
     if (window < 0 || num_sinks < 0) return PSA_ERR_INVALID_ARG;
+    if ((long long)d->batch * d->num_kv_heads > (1 << 23) || (long long)d->batch * d->num_q_heads > (1 << 24)) return PSA_ERR_UNSUPPORTED;
     return d->max_blocks_per_seq > INT32_MAX / psa::kPage ? PSA_ERR_UNSUPPORTED : PSA_OK;
 }
 
@@ -298,10 +299,10 @@ psa_status check_packed(const psa_kv_desc *d, const void *packed, bool need_tabl
     return PSA_OK;
 }
 
-// As for the metadata: how many pages are listed.  `nothing`: there is nothing to do.
+// As for the metadata: how many pages are listed, a wave for each and KV head.  `nothing`: there is nothing to do.
 psa_status check_list(const psa_kv_desc *d, const int32_t *page_list, int32_t num_listed, bool *nothing) {
     if (num_listed < 0 || (num_listed > 0 && !page_list)) return PSA_ERR_INVALID_ARG;
-    if ((long long)(page_list ? num_listed : d->num_pages) * d->num_kv_heads > INT32_MAX) return PSA_ERR_UNSUPPORTED;
+    if ((long long)(page_list ? num_listed : d->num_pages) * d->num_kv_heads > (1 << 25)) return PSA_ERR_UNSUPPORTED;
     *nothing = (page_list && num_listed == 0) || d->num_pages == 0;
     return PSA_OK;
 }
@@ -386,6 +387,7 @@ psa_status psa_norm_rotate(const psa_rotate_desc *d, const void *q_in, const voi
     if (!d || d->num_tokens < 0 || d->num_q_heads < 0 || d->num_kv_heads < 0) return PSA_ERR_INVALID_ARG;
     if (d->dtype != PSA_F16 && d->dtype != PSA_BF16) return PSA_ERR_UNSUPPORTED;
     if (d->head_dim != psa::kHeadDim || d->num_q_heads > 65536 || d->num_kv_heads > 65536) return PSA_ERR_UNSUPPORTED;
+    if (d->num_tokens > (1 << 25)) return PSA_ERR_UNSUPPORTED;              // (a wave for each)
     if (d->rot_dim < 0 || d->rot_dim > d->head_dim || d->rot_dim % 8 != 0) return PSA_ERR_INVALID_ARG;
     if (d->interleaved < 0 || d->interleaved > 1 || d->normalize < 0 || d->normalize > 1) return PSA_ERR_INVALID_ARG;
     if (!(d->eps >= 0.0f) || isinf(d->eps)) return PSA_ERR_INVALID_ARG;      // also rejects NaN

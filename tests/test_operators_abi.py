@@ -110,6 +110,18 @@ def test_page_calls_refuse(lib):
     assert append(_desc(batch=0), k=None, v=None) == OK
 
 
+def test_calls_of_more_threads_than_a_launch_has_are_refused(lib):
+    for kw in (dict(batch=(1 << 23) // 8 + 1), dict(batch=(1 << 24) // 64 + 1, num_q_heads=64)):
+        d = _desc(**kw)
+        assert _window(lib, d) == UNSUPPORTED and _packed(lib, d) == UNSUPPORTED
+        assert lib.psa_window_workspace_bytes(C.byref(d), 5000, 0) == 0 and lib.psa_packed_workspace_bytes(C.byref(d), 5000, 0) == 0
+        assert lib.psa_append_kv_packed(C.byref(d), 0x1000, 0x10, 0x20, None, None) == UNSUPPORTED
+    for call in (lambda n: lib.psa_pack_pages(C.byref(_desc()), 0x1000, None, 0x10, n, None),
+                 lambda n: lib.psa_unpack_pages(C.byref(_desc()), 0x1000, 0x10, n, None)):
+        assert call((1 << 25) // 8 + 1) == UNSUPPORTED
+    assert _rotate(lib, num_tokens=(1 << 25) + 1) == UNSUPPORTED
+
+
 def test_packed_calls_refuse_a_second_tier(lib):
     tier = pb._Tier(0x1000, 0x2000, 1 << 20, 64, 0, None, 0)
     d = _desc(tier=C.addressof(tier))
