@@ -232,7 +232,7 @@ __global__ __launch_bounds__(256, 3) void packed_kernel(KvView kv, const uint8_t
     const int b0 = piece.b0, b1 = plan.direct ? vis.count : piece.b1;
 
     const int hd = cl / kRows, part = cl % kRows;
-    const WeightParts<1, G> parts(part);
+    const WeightParts<G> parts(part);
     uint4 qb[4];                                         // B operand of the logits: channels 32 rg + 8 kk .. + 7
 #pragma unroll
     for (int kk = 0; kk < 4; ++kk) {
@@ -304,9 +304,9 @@ __global__ __launch_bounds__(256, 3) void packed_kernel(KvView kv, const uint8_t
 #pragma unroll
         for (int j = 0; j < 8; ++j) p[j] = exp2_fast(fmaf(sc[j], kScaleLog2, -ref));
         l += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
-        uint4 a[kProducts<1, G>];
+        uint4 a[kProducts<G>];
 #pragma unroll
-        for (int y = 0; y < kProducts<1, G>; ++y)
+        for (int y = 0; y < kProducts<G>; ++y)
             a[y] = make_uint4(parts(p[0], p[1], y), parts(p[2], p[3], y), parts(p[4], p[5], y), parts(p[6], p[7], y));
         float power[8];
 #pragma unroll
@@ -321,7 +321,7 @@ __global__ __launch_bounds__(256, 3) void packed_kernel(KvView kv, const uint8_t
             const uint4 odd = make_uint4(pick_halves<true>(x[0], x[1]), pick_halves<true>(x[2], x[3]),
                                          pick_halves<true>(x[4], x[5]), pick_halves<true>(x[6], x[7]));
 #pragma unroll
-            for (int y = 0; y < kProducts<1, G>; ++y) {
+            for (int y = 0; y < kProducts<G>; ++y) {
                 acc[2 * u] = mfma_16x16x32<1>(a[y], even, acc[2 * u]);
                 acc[2 * u + 1] = mfma_16x16x32<1>(a[y], odd, acc[2 * u + 1]);
             }
@@ -343,7 +343,7 @@ __global__ __launch_bounds__(256, 3) void packed_kernel(KvView kv, const uint8_t
     }
     l += __shfl_xor(l, 16);
     l += __shfl_xor(l, 32);
-    store_parts<1, G>(acc, sums.acc[wave], rg, cl);
+    store_parts<G>(acc, sums.acc[wave], rg, cl);
     if (rg == 0 && hd < G && part == 0) { sums.m[wave][hd] = limit == -INFINITY ? -INFINITY : ref; sums.l[wave][hd] = l; }
     const bool bad_ctx = __ballot(err & PSA_DEVERR_CTX_RANGE) != 0ull, bad_page = __ballot(err & PSA_DEVERR_PAGE_RANGE) != 0ull;
     if (lane == 0) sums.err[wave] = (bad_ctx ? PSA_DEVERR_CTX_RANGE : 0) | (bad_page ? PSA_DEVERR_PAGE_RANGE : 0);

@@ -36,39 +36,31 @@ __device__ __forceinline__ Visible make_visible(int ctx, int window, int num_sin
     return v;
 }
 
-// The weights of the value product, p in (0, 2^kSlack], are given to the matrix cores in 16-bit parts in neighbouring rows of one
-// operand: upper and lower half in binary16 (22 bits of p), three parts in bfloat16 (all 24 bits: each is what truncation
-// leaves of the rest).  Two bfloat16 parts leave an error of about 1e-6 of the output; three cost nothing where a head has four rows,
-// and a second product of the same values where it has two (eight heads).
+// The weights of the value product, p in [0, 2^kSlack], are given to the matrix cores in three bfloat16 parts (all 24 bits: each is
+// what truncation leaves of the rest) in neighbouring rows of one operand.  bfloat16 whatever the cache's type, because a weight
+// far below the reference counts as much as its value makes it: where a first token holds nearly everything and its value is near
+// zero, the output is made of weights of 2^-20 and less, of which binary16 would lose the lower bits, and below 2^-25 all of them
+// (65536 tokens 25.5 octaves below the first lost a quarter of the output).  Two bfloat16 parts leave an error of about 1e-6 of the output;
+// three cost nothing where a head has four rows, and a second product of the same values where it has two (eight heads).
 template <int G>
 constexpr int kRowsPerHead = G == 8 ? 2 : 4;
-template <int DT, int G>
-constexpr int kProducts = (DT == 1 && G == 8) ? 2 : 1;
+template <int G>
+constexpr int kProducts = G == 8 ? 2 : 1;
 
 // The part of two weights that the lane's row gets in product `which`, packed.  What to take off is a mask per lane, so that
-// nothing branches: bfloat16 parts are p, p less its upper 16 bits, and that less its own upper 16 bits, each cut to 16 bits
-// (a row beyond the parts gets the last part again, and store_parts leaves it out).  Binary16 parts are p cut to 11
-// bits, exactly, and the rest, rounded.
-template <int DT, int G>
+// nothing branches: the parts are p, p less its upper 16 bits, and that less its own upper 16 bits, each cut to 16 bits
+// (a row beyond the parts gets the last part again, and store_parts leaves it out).
+template <int G>
 struct WeightParts {
     uint32_t m1, m2;
     __device__ __forceinline__ explicit WeightParts(int part) {
-        if constexpr (DT == 0) {
-            m1 = part == 0 ? 0xffffe000u : ~0u;
-            m2 = part == 0 ? 0u : 0xffffe000u;
-        } else if constexpr (G == 8) {
-            m1 = part == 0 ? 0u : 0xffff0000u;
-            m2 = part == 0 ? 0xffff0000u : 0u;
-        } else {
-            m1 = part == 0 ? 0u : 0xffff0000u;
-            m2 = part < 2 ? 0u : 0xffff0000u;
-        }
+        m1 = part == 0 ? 0u : 0xffff0000u;
+        if constexpr (G == 8) m2 = part == 0 ? 0xffff0000u : 0u;
+        else m2 = part < 2 ? 0u : 0xffff0000u;
     }
     __device__ __forceinline__ static float masked(float x, uint32_t m) { return __uint_as_float(__float_as_uint(x) & m); }
     __device__ __forceinline__ float pick(float p, int which) const {
-        if constexpr (DT == 0) {
-            return masked(p, m1) - masked(p, m2);
-        } else if constexpr (G == 8) {
+        if constexpr (G == 8) {
             if (which == 0) return p - masked(p, m1);
             const float r = p - masked(p, 0xffff0000u);
             return masked(r - masked(r, 0xffff0000u), m2);
@@ -77,18 +69,12 @@ struct WeightParts {
             return r - masked(r, m2);
         }
     }
-    __device__ __forceinline__ uint32_t operator()(float p0, float p1, int which) const {
-        const float a = pick(p0, which), b = pick(p1, which);
-        if constexpr (DT == 0) {
-            const half2_t h = {(_Float16)a, (_Float16)b};
-            return __builtin_bit_cast(uint32_t, h);
-        } else {
-            return upper_halves(a, b);
-        }
-    }
+    __device__ __forceinline__ uint32_t operator()(float p0, float p1, int which) const { return upper_halves(pick(p0, which), pick(p1, which)); }
     __device__ __forceinline__ static uint32_t upper_halves(float a, float b) {
         return __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u);
     }
+    // what its upper 16 bits leave of a number
+    __device__ __forceinline__ static float rest(float x) { return x - masked(x, 0xffff0000u); }
 };
 // The lower (or upper) 16-bit halves of two words, packed.
 template <bool UPPER>
@@ -97,7 +83,7 @@ __device__ __forceinline__ uint32_t pick_halves(uint32_t a, uint32_t b) {
 }
 
 // The lane's sums, rows 4 rg .. 4 rg + 3 of channels 8 cl .. 8 cl + 7, to rows[head][channel]: the parts of a head are added.
-template <int DT, int G>
+template <int G>
 __device__ __forceinline__ void store_parts(const f32x4_t (&acc)[8], float (*rows)[kHeadDim], int rg, int cl) {
     constexpr int kHeads = 4 / kRowsPerHead<G>;
 #pragma unroll
@@ -112,7 +98,6 @@ __device__ __forceinline__ void store_parts(const f32x4_t (&acc)[8], float (*row
                 for (int t = 0; t < 4; ++t) {
                     const f32x4_t &a = acc[4 * y + t];
                     if constexpr (G == 8) o[t] = a[2 * k] + a[2 * k + 1];
-                    else if constexpr (DT == 0) o[t] = a[0] + a[1];
                     else o[t] = a[0] + (a[1] + a[2]);
                 }
                 row[y] = o;

@@ -10,7 +10,8 @@ namespace psa {
 // grid: one workgroup of four waves per piece (or request) and KV head, before them the one that checks the tables (if any).
 // A wave takes every fourth visible block and carries its own online softmax over them: logits with four 16x16x32 products,
 // lane (kq, n) = (lane / 16, lane % 16) getting the logits of the head of row n for tokens kq, 4+kq, 8+kq, 12+kq; values with eight
-// 16x16x16 products, the weights in parts in a head's rows.  Tokens of a block that the query does not see get the logit -inf and a
+// 16x16x16 products, the weights in parts in a head's rows; values in binary16 are split into two bfloat16 parts, exactly, that share
+// one 16x16x32 product with the weights twice.  Tokens of a block that the query does not see get the logit -inf and a
 // zero value row (the page may hold NaN there).
 // Bound by memory: 4 requests of 64K tokens, 8 KV heads, G = 4: 165 us a call = 6.5 TB/s; 64 ragged requests with a window of 4096
 // and 16 sinks, G = 8: 160 us = 6.4; 240 ragged ones with a window of 130, 4 KV heads: 17 us = 3.8, of which 5 are the way to the first
@@ -44,7 +45,7 @@ __global__ __launch_bounds__(256, 3) void window_kernel(KvView kv, const uint8_t
     const int b0 = piece.b0, b1 = plan.direct ? vis.count : piece.b1;
 
     const int hd = cl / kRows, part = cl % kRows;
-    const WeightParts<DT, G> parts(part);
+    const WeightParts<G> parts(part);
     uint4 qb[4];                                         // B operand of the logits: a head's rows all hold its query
 #pragma unroll
     for (int kk = 0; kk < 4; ++kk) {
@@ -97,21 +98,32 @@ __global__ __launch_bounds__(256, 3) void window_kernel(KvView kv, const uint8_t
 #pragma unroll
         for (int j = 0; j < 4; ++j) p[j] = exp2_fast(sc[j] - ref);
         l += (p[0] + p[1]) + (p[2] + p[3]);
-        uint2 a[kProducts<DT, G>];
+        uint2 a[kProducts<G>];
 #pragma unroll
-        for (int y = 0; y < kProducts<DT, G>; ++y) a[y] = make_uint2(parts(p[0], p[1], y), parts(p[2], p[3], y));
+        for (int y = 0; y < kProducts<G>; ++y) a[y] = make_uint2(parts(p[0], p[1], y), parts(p[2], p[3], y));
         static_for<8>([&](auto t) __attribute__((always_inline)) {
             constexpr int w = t / 2;
             constexpr bool odd = t & 1;
-            const uint2 bv = make_uint2(pick_halves<odd>(pick_word(v.r[0], w), pick_word(v.r[1], w)),
-                                        pick_halves<odd>(pick_word(v.r[2], w), pick_word(v.r[3], w)));
+            if constexpr (DT == 1) {
+                const uint2 bv = make_uint2(pick_halves<odd>(pick_word(v.r[0], w), pick_word(v.r[1], w)),
+                                            pick_halves<odd>(pick_word(v.r[2], w), pick_word(v.r[3], w)));
 #pragma unroll
-            for (int y = 0; y < kProducts<DT, G>; ++y) acc[t] = mfma_16x16x16<DT>(a[y], bv, acc[t]);
+                for (int y = 0; y < kProducts<G>; ++y) acc[t] = mfma_16x16x16<1>(a[y], bv, acc[t]);
+            } else {                                     // the weights with the values' upper parts, and again with the rest
+                float x[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) x[j] = odd ? cvt_hi<0>(pick_word(v.r[j], w)) : cvt_lo<0>(pick_word(v.r[j], w));
+                using W = WeightParts<G>;
+                const uint4 bv = make_uint4(W::upper_halves(x[0], x[1]), W::upper_halves(x[2], x[3]),
+                                            W::upper_halves(W::rest(x[0]), W::rest(x[1])), W::upper_halves(W::rest(x[2]), W::rest(x[3])));
+#pragma unroll
+                for (int y = 0; y < kProducts<G>; ++y) acc[t] = mfma_16x16x32<1>(make_uint4(a[y].x, a[y].y, a[y].x, a[y].y), bv, acc[t]);
+            }
         });
     }
     l += __shfl_xor(l, 16);
     l += __shfl_xor(l, 32);
-    store_parts<DT, G>(acc, sums.acc[wave], rg, cl);
+    store_parts<G>(acc, sums.acc[wave], rg, cl);
     if (rg == 0 && hd < G && part == 0) { sums.m[wave][hd] = limit == -INFINITY ? -INFINITY : ref; sums.l[wave][hd] = l; }
     const bool bad_ctx = __ballot(err & PSA_DEVERR_CTX_RANGE) != 0ull, bad_page = __ballot(err & PSA_DEVERR_PAGE_RANGE) != 0ull;
     if (lane == 0) sums.err[wave] = (bad_ctx ? PSA_DEVERR_CTX_RANGE : 0) | (bad_page ? PSA_DEVERR_PAGE_RANGE : 0);
