@@ -430,13 +430,17 @@ def _device_of(t: torch.Tensor) -> int:
     return at
 
 
+def _same_device(stream, at: int) -> None:
+    if stream.device.index != at:
+        raise ValueError(f"the stream is of {stream.device}, the tensors are on cuda:{at}")
+
+
 def _launch(call, at: int, stream, *args) -> None:
     """call(*args, stream) with the tensors' device as the current one, on the caller's stream or that device's current one."""
     if stream is None:
         handle = _raw_stream(at)
-    elif stream.device.index != at:
-        raise ValueError(f"the stream is of {stream.device}, the tensors are on cuda:{at}")
     else:
+        _same_device(stream, at)
         handle = stream.cuda_stream
     if _current_device() == at:
         status = call(*args, handle)
@@ -458,19 +462,30 @@ def _tensor(name: str, t: torch.Tensor, shape: tuple, dtype, at: int) -> int:
     _refuse(name, t, f"a contiguous {dtype} tensor of shape {tuple(shape)} on device {at}")
 
 
+def _new(at: int, stream, *wanted) -> list:
+    """Buffers that a call makes, (shape, type) each, for kernels on `stream`.  They come from that stream's memory: what the
+    allocator has free on another stream may still be in use by work queued there.  Nor are they given back before the work
+    queued on the current stream is done, which is where they are read as a rule."""
+    if stream is None:
+        return [torch.empty(shape, dtype=dtype, device=f"cuda:{at}") for shape, dtype in wanted]
+    _same_device(stream, at)
+    here = torch.cuda.current_stream(at)
+    with torch.cuda.stream(stream):
+        made = [torch.empty(shape, dtype=dtype, device=f"cuda:{at}") for shape, dtype in wanted]
+    for t in made:
+        t.record_stream(here)
+    return made
+
+
 def _results(q: torch.Tensor, workspace, nbytes, out, lse, stream):
-    """The caller's buffers, and new ones where there are none (not given back to the allocator before `stream` is done with them)."""
-    made = []
-    if workspace is None:
-        made.append(workspace := torch.empty(nbytes, dtype=torch.uint8, device=q.device))
+    """The caller's buffers, and new ones where there are none."""
+    wanted = [] if workspace is not None else [((nbytes,), torch.uint8)]
     if out is None:
-        made.append(out := torch.empty(q.shape, dtype=torch.float32, device=q.device))
+        wanted.append((q.shape, torch.float32))
     if lse is None:
-        made.append(lse := torch.empty(q.shape[:2], dtype=torch.float32, device=q.device))
-    if stream is not None:
-        for t in made:
-            t.record_stream(stream)
-    return workspace, out, lse
+        wanted.append((q.shape[:2], torch.float32))
+    made = iter(_new(q.get_device(), stream, *wanted))
+    return next(made) if workspace is None else workspace, next(made) if out is None else out, next(made) if lse is None else lse
 
 
 def _scratch(workspace: torch.Tensor, at: int) -> int:
@@ -617,14 +632,8 @@ def norm_rotate(q: torch.Tensor, k: torch.Tensor, positions: torch.Tensor, inv_f
     T, Hq, _ = q.shape
     q_shape, k_shape, half = (T, Hq, 128), (T, k.shape[1], 128), inv_freq.numel()
     if q_out is None or k_out is None:
-        made = []
-        if q_out is None:
-            made.append(q_out := torch.empty(q_shape, dtype=dtype, device=q.device))
-        if k_out is None:
-            made.append(k_out := torch.empty(k_shape, dtype=dtype, device=q.device))
-        if stream is not None:
-            for t in made:
-                t.record_stream(stream)
+        made = iter(_new(at, stream, *([(q_shape, dtype)] if q_out is None else []), *([(k_shape, dtype)] if k_out is None else [])))
+        q_out, k_out = next(made) if q_out is None else q_out, next(made) if k_out is None else k_out
     if not normalize:
         q_weight = k_weight = None
     d = _RotateDesc(T, Hq, k_shape[1], 128, 2 * half, bool(interleaved), bool(normalize), _dtype_code(dtype), _rows("q", q, q_shape, dtype, at),
