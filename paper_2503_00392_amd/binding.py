@@ -536,20 +536,32 @@ def window_attention(kv: KvCache, q: torch.Tensor, window: int, num_sinks: int =
 
 class PackedCache:
     """One layer's paged cache in 4 bits and its tables: pool uint8 [P][Hkv][2176], block_table int32 [B][max_blocks],
-    ctx_lens int32 [B], queries and new tokens of `dtype`.  The descriptor is made once: the tensors stay in place."""
+    ctx_lens int32 [B], queries and new tokens of `dtype`.  Any of them may be assigned anew, as with KvCache: the descriptor is made
+    once and again after an assignment, at the next call, which refuses tensors that do not belong together."""
 
     def __init__(self, pool: torch.Tensor, block_table: torch.Tensor, ctx_lens: torch.Tensor, num_q_heads: int, dtype: torch.dtype):
-        if pool.dim() != 3 or block_table.dim() != 2:
+        self.pool, self.block_table, self.ctx_lens, self.num_q_heads, self.dtype = pool, block_table, ctx_lens, int(num_q_heads), dtype
+        self._made()
+
+    def __setattr__(self, name, value):
+        super().__setattr__(name, value)
+        if name in ("pool", "block_table", "ctx_lens", "num_q_heads", "dtype"):
+            self._desc = None
+
+    @property
+    def num_kv_heads(self) -> int:
+        return int(self.pool.shape[1])
+
+    def _made(self) -> _KvDesc:
+        pool, table, lens = self.pool, self.block_table, self.ctx_lens
+        if pool.dim() != 3 or table.dim() != 2:
             raise ValueError("pool: [num_pages][num_kv_heads][2176], block_table: [batch][max_blocks]")
-        at = pool.get_device()
-        _tensor("pool", pool, (pool.shape[0], pool.shape[1], PACKED_RECORD_BYTES), torch.uint8, at)
-        _tensor("block_table", block_table, block_table.shape, torch.int32, at)
-        _tensor("ctx_lens", ctx_lens, (block_table.shape[0],), torch.int32, at)
-        self.pool, self.block_table, self.ctx_lens = pool, block_table, ctx_lens
-        self.num_q_heads, self.num_kv_heads, self.dtype = int(num_q_heads), int(pool.shape[1]), dtype
-        self._desc = _KvDesc(block_table.shape[0], self.num_q_heads, self.num_kv_heads, 128, 16, pool.shape[0],
-                             block_table.shape[1], _dtype_code(dtype), None, None, _ptr(block_table), _ptr(ctx_lens), None)
-        self._q_shape, self._kv_shape = ((block_table.shape[0], n, 128) for n in (self.num_q_heads, self.num_kv_heads))
+        at, (P, H, _), (B, width) = pool.get_device(), pool.shape, table.shape
+        _tensor("pool", pool, (P, H, PACKED_RECORD_BYTES), torch.uint8, at)
+        where = _tensor("block_table", table, (B, width), torch.int32, at), _tensor("ctx_lens", lens, (B,), torch.int32, at)
+        desc = _KvDesc(B, self.num_q_heads, H, 128, 16, P, width, _dtype_code(self.dtype), None, None, *where, None)
+        self._desc, self._q_shape, self._kv_shape = desc, (B, self.num_q_heads, 128), (B, H, 128)
+        return desc
 
     @staticmethod
     def empty_pool(num_pages: int, num_kv_heads: int, device="cuda") -> torch.Tensor:
@@ -589,24 +601,26 @@ def unpack_pages(kv: KvCache, packed: torch.Tensor, page_list=None, stream=None)
 def append_kv_packed(cache: PackedCache, k_new: torch.Tensor, v_new: torch.Tensor, status: torch.Tensor | None = None,
                      stream=None) -> None:
     """psa_append_kv_packed: writes into cache.pool and cache.ctx_lens in place."""
+    desc = cache._desc or cache._made()
     at, shape = _device_of(cache.pool), cache._kv_shape
-    _launch(load_library().psa_append_kv_packed, at, stream, cache._desc, cache.pool.data_ptr(), _tensor("k_new", k_new, shape, cache.dtype, at),
+    _launch(load_library().psa_append_kv_packed, at, stream, desc, cache.pool.data_ptr(), _tensor("k_new", k_new, shape, cache.dtype, at),
             _tensor("v_new", v_new, shape, cache.dtype, at), None if status is None else _tensor("status", status, shape[:1], torch.int32, at))
 
 
 def packed_workspace_bytes(cache: PackedCache, window: int = EVERYTHING, num_sinks: int = 0) -> int:
-    return int(load_library().psa_packed_workspace_bytes(cache._desc, _tokens(window), _tokens(num_sinks)))
+    return int(load_library().psa_packed_workspace_bytes(cache._desc or cache._made(), _tokens(window), _tokens(num_sinks)))
 
 
 def packed_attention(cache: PackedCache, q: torch.Tensor, window: int = EVERYTHING, num_sinks: int = 0, *,
                      workspace: torch.Tensor | None = None, out: torch.Tensor | None = None, lse: torch.Tensor | None = None,
                      stream=None):
     """psa_packed_attention; returns (out float32 [B][Hq][128], lse float32 [B][Hq])."""
+    desc = cache._desc or cache._made()
     at, shape, window, num_sinks = _device_of(cache.pool), cache._q_shape, _tokens(window), _tokens(num_sinks)
     where = _tensor("q", q, shape, cache.dtype, at)
     if workspace is None or out is None or lse is None:
         workspace, out, lse = _results(q, workspace, 0 if workspace is not None else packed_workspace_bytes(cache, window, num_sinks), out, lse, stream)
-    _launch(load_library().psa_packed_attention, at, stream, cache._desc, cache.pool.data_ptr(), where, window, num_sinks,
+    _launch(load_library().psa_packed_attention, at, stream, desc, cache.pool.data_ptr(), where, window, num_sinks,
             _tensor("out", out, shape, torch.float32, at), _tensor("lse", lse, shape[:2], torch.float32, at), _scratch(workspace, at), workspace.nbytes)
     out._workspace = workspace
     return out, lse
