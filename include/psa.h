@@ -320,7 +320,10 @@ psa_status psa_window_attention(const psa_kv_desc *desc, const void *q, int32_t 
  * The paged cache in 4 bits: 2176 bytes where the 16-bit cache has 8192.  An element is e2m1 (a sign and one of 0, 0.5, 1,
  * 1.5, 2, 3, 4, 6); 32 channels of a token share a power of two, stored as the byte e + 127: the smallest e >= -126 with
  * max|x| <= 7 * 2^e.  Elements are x / 2^e to the nearest, ties to even, 6 at most.  A block of 32 with an infinity or a NaN has
- * the byte 255 and reads as NaN.  The packed pool is [num_pages][num_kv_heads] records of PSA_PACKED_RECORD_BYTES, 16-byte aligned:
+ * the byte 255 and reads as NaN.  The top of a type's range stands for more than the type holds: binary16 numbers above 57344 are
+ * stored as 65536, which psa_unpack_pages gives back as an infinity in binary16 (to attention it is 65536), bfloat16 numbers above
+ * 1.75 * 2^127 as 2^128, which is an infinity to both (NaN or infinite in outputs).  Numbers stored as 2^-127 (below 2^-126) may read
+ * as zeros.  The packed pool is [num_pages][num_kv_heads] records of PSA_PACKED_RECORD_BYTES, 16-byte aligned:
  *      0  keys' elements [token][channel / 2], the even channel in the low half of the byte
  *   1024  values' elements [token / 4][channel / 8][token % 4][channel % 8 / 2]
  *   2048  keys' exponents [token][channel / 32]
@@ -332,7 +335,7 @@ psa_status psa_window_attention(const psa_kv_desc *desc, const void *q, int32_t 
  *   tokens beyond a page's fill are written as zeros and not looked at.  A call takes up to 2^25 pages times KV heads
  *   (beyond: PSA_ERR_UNSUPPORTED), psa_unpack_pages also.
  * psa_unpack_pages: records to pages of the 16-bit cache (WRITES desc->k_pool and desc->v_pool), rounded to desc->dtype: exact in
- *   bfloat16.  page_list, num_listed as above.
+ *   bfloat16 from 2^-126 to below 2^128; in binary16 infinite from 65536 on.  page_list, num_listed as above.
  * psa_append_kv_packed: as psa_append_kv, with the token going to the packed pool, bit for bit as psa_pack_pages packs
  *   it (no metadata is kept); k_new and v_new [batch][num_kv_heads][head_dim] of desc->dtype, 16-byte aligned.
  * psa_packed_attention: as psa_window_attention over the packed cache; q of desc->dtype; the dense form is a window of INT32_MAX.

@@ -7,6 +7,8 @@
 // is from its neighbours in the elements' last octave, so nothing loses more by saturation than by rounding.  A power of two
 // for 32 channels and a rounding to the nearest element mean: an element is off by at most 2^e / 4 below 2 * 2^e, by 2^e / 2
 // below 4 * 2^e and by 2^e above.  A block with an infinity or a NaN gets the byte 255 and reads as NaN.
+// What is above 7/8 of a type's last power of two gets the element that stands for that power: 65536 for binary16 numbers above 57344 (an
+// infinity when read back to binary16), 2^128 for bfloat16 ones above 1.75 * 2^127 (an infinity in any case).
 //
 // Record of one (page, KV head), 2176 bytes = 17 lines of 128:
 //      0  keys' elements [token][channel / 2], even channel in the low half
@@ -55,7 +57,7 @@ __device__ __forceinline__ uint32_t to_elements(const uint4 &w, uint32_t byte) {
     }
     return byte == 255u ? 0u : c;
 }
-// Eight elements to eight 16-bit values (exact in bfloat16).
+// Eight elements to eight 16-bit values: exact in bfloat16 from 2^-126 to below 2^128, infinite in binary16 from 65536 on.
 template <int DT>
 __device__ __forceinline__ uint4 from_elements(uint32_t c, float s) {
     if constexpr (DT == 0) {
