@@ -697,6 +697,9 @@ def tier_update(kv: KvCache, order: torch.Tensor, blocks_read: torch.Tensor, bus
 
 
 def read_device_error(workspace: torch.Tensor, stream=None) -> int:
+    """psa_read_device_error, after what is queued on `stream` (the current one of the workspace's GPU if none is given)."""
+    if stream is None:
+        stream = torch.cuda.current_stream(workspace.device)
     flags = C.c_int32(0)
     st = load_library().psa_read_device_error(_ptr(workspace), C.byref(flags), _stream(stream))
     _check(st, "psa_read_device_error")

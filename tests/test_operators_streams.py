@@ -61,6 +61,23 @@ def test_buffers_come_from_the_stream_that_writes_them(monkeypatch, name, given)
         assert not made
 
 
+def test_the_error_word_is_read_behind_the_calls_of_its_own_gpu(monkeypatch):
+    """The calls run on the current stream of the tensors' GPU, whichever GPU is the current one; so does the read of their error word."""
+    asked = []
+
+    def current_stream(device=None):
+        asked.append(device)
+        return types.SimpleNamespace(cuda_stream=1)
+
+    class Library:
+        psa_read_device_error = staticmethod(lambda workspace, flags, stream: pb.PSA_OK)
+
+    monkeypatch.setattr(torch.cuda, "current_stream", current_stream)
+    monkeypatch.setattr(pb, "load_library", lambda: Library)
+    workspace = torch.empty(256, dtype=torch.uint8, device="meta")
+    assert psa.read_device_error(workspace) == 0 and asked == [workspace.device]
+
+
 @pytest.mark.gpu
 @pytest.mark.parametrize("name", ["window", "packed", "rotate"])
 def test_memory_let_go_behind_running_work_is_not_written(name):
