@@ -81,7 +81,22 @@ __global__ __launch_bounds__(256) void rotate_kernel(RotateArgs a) {
             float sum = 0.0f;
 #pragma unroll
             for (int j = 0; j < 8; ++j) sum = fmaf(x[j], x[j], sum);
-            const float f = 1.0f / sqrtf(row_sum16(sum) * (1.0f / kHeadDim) + a.eps);
+            sum = row_sum16(sum);
+            float eps = a.eps;
+            // Squares beyond binary32 (bfloat16 numbers above 2^60; below 2^-50 if eps is as good as none): the row and eps are
+            // scaled by a power of two first, which the quotient does not see.  All lanes of a row go the same way.
+            if (!(sum < INFINITY) || sum + kHeadDim * eps < 0x1p-90f) {
+                const float scale = sum > 1.0f ? 0x1p-80f : 0x1p80f;
+                sum = 0.0f;
+#pragma unroll
+                for (int j = 0; j < 8; ++j) {
+                    x[j] *= scale;
+                    sum = fmaf(x[j], x[j], sum);
+                }
+                sum = row_sum16(sum);
+                eps = eps * scale * scale;
+            }
+            const float f = 1.0f / sqrtf(sum * (1.0f / kHeadDim) + eps);
             const uint8_t *w = is_q ? a.q_weight : a.k_weight;
             float g[8] = {1.0f, 1.0f, 1.0f, 1.0f, 1.0f, 1.0f, 1.0f, 1.0f};
             if (w) {
