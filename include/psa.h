@@ -301,11 +301,12 @@ psa_status psa_dense_attention(const psa_kv_desc *desc, const void *q, float *ou
  *   window, num_sinks  >= 0, in tokens, of any size: a window of INT32_MAX attends everything, a window of 0 the sinks
  *                      alone, both 0 nothing
  *   out  [batch][num_q_heads][head_dim] float32; lse [batch][num_q_heads] float32 natural-log sum of exponentiated scaled
- *        logits, may be NULL.  Where nothing is visible out = 0 and lse = -inf; a NaN in a visible key or value shows in the
+ *        logits, may be NULL.  Where nothing is visible, or nothing but logits of -inf, out = 0 and lse = -inf; a NaN in a visible key or value shows in the
  *        outputs of its heads, an infinity in a visible value gives infinities or NaN
  *   workspace  psa_window_workspace_bytes of the same descriptor, window and num_sinks; holds the sticky error word
- * A call repeated gives the same bits.  How a request is cut, and with it the order of its sums, follows from the lengths of all
- * requests of the batch: its results can differ in the last bits from those it has in another batch.
+ * A call repeated gives the same bits.  How a request is cut, and with it the order of its sums, follows from the batch, the lengths of
+ * all its requests, the width of the block table (max_blocks_per_seq), the head counts, window and num_sinks: its results can differ in
+ * the last bits from those it has in another batch or with a wider table.
  * Pages without a visible token are not looked at, nor are their block-table entries: they may have been freed.  What a
  * page holds beside the visible tokens does not matter (NaN included).
  * Shapes as for psa_dense_attention, max_blocks_per_seq up to 2^27 - 1, batch * num_kv_heads up to 2^23, batch * num_q_heads
@@ -337,7 +338,8 @@ psa_status psa_window_attention(const psa_kv_desc *desc, const void *q, int32_t 
  * psa_unpack_pages: records to pages of the 16-bit cache (WRITES desc->k_pool and desc->v_pool), rounded to desc->dtype: exact in
  *   bfloat16 from 2^-126 to below 2^128; in binary16 infinite from 65536 on.  page_list, num_listed as above.
  * psa_append_kv_packed: as psa_append_kv, with the token going to the packed pool, bit for bit as psa_pack_pages packs
- *   it (no metadata is kept); k_new and v_new [batch][num_kv_heads][head_dim] of desc->dtype, 16-byte aligned.
+ *   it (no metadata is kept); k_new and v_new [batch][num_kv_heads][head_dim] of desc->dtype, 16-byte aligned.  Like psa_append_kv it
+ *   raises desc->ctx_lens: two caches that are both appended to have lengths of their own.
  * psa_packed_attention: as psa_window_attention over the packed cache; q of desc->dtype; the dense form is a window of INT32_MAX.
  *   Elements are used as the values they stand for, with nothing rounded but the result's binary32 sums.
  */
@@ -358,7 +360,7 @@ psa_status psa_packed_attention(const psa_kv_desc *desc, const void *packed_pool
  *   y = x / sqrt(mean(x^2) + eps) * w     with desc->normalize, w = the weights or 1; y = x without
  *   pair i < rot_dim / 2 of y:  (a, b) -> (a cos u - b sin u, a sin u + b cos u),  u = position * inv_freq[i]
  * The pair is (y[i], y[i + rot_dim / 2]), or (y[2 i], y[2 i + 1]) with desc->interleaved; channels from rot_dim on are not
- * rotated.  Computed in binary32 (the angle in binary64) and rounded once.
+ * rotated.  Computed in binary32 (the angle in binary64; rows whose squares leave its range are scaled first) and rounded once.
  *   q_in, k_in    [num_tokens][heads][head_dim] of desc->dtype, q_in_stride and k_in_stride elements from token to token (so
  *                 both may lie in one projection's output); q_out, k_out likewise.  An output may be its own input, with the
  *                 same stride; otherwise buffers do not overlap.

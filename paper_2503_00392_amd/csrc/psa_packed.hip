@@ -203,7 +203,7 @@ __device__ __forceinline__ uint32_t word_of(const uint4 &v, int w) { return w ==
 //           tokens.  Lane (rg, cl) has the logits of tokens 4 rg .. + 3 of both pages and loads just those tokens' values.
 // (The matrix cores also take 4-bit elements and their powers as they are, with 8-bit floating parts of the query, but then
 // add 128 products of different sizes with an error of 1e-5 of the sum of these sizes in the mean; these sums leave 1e-7.)
-// Bound by memory: 4 requests of 128K tokens, 8 KV heads: 93 us = 6.1 TB/s at G = 4 (the call, with the launch that joins, 100),
+// Bound by memory: 4 requests of 128K tokens, 8 KV heads: 91 us = 6.3 TB/s at G = 4 (the call, with the launch that joins, 95),
 // vector ALUs 46 % busy -- 64 conversions, 36 permutations and some 100 others for a pair of blocks --, matrix cores 12 %.  What brought
 // it there from 173 us: the next pair under way (140), weight parts by masks and not by branches (127), table entries from
 // a list that is loaded 64 blocks ahead and not each before its page (103).  Three pairs under way take as long; a workgroup needs

@@ -11,7 +11,8 @@
 // rot_dim fills the remaining places and passes through.
 // Bound by memory for prompts (256 bytes in and out for a row): 16384 tokens of 32 + 8 heads 69 us = 4.9 TB/s, a large copy's rate
 // (75 us without the streaming hints and one row at a time).  One token 3.1 us, of which the launch is most: its ten waves take four
-// rows each (7.0 us with one wave for all forty, one after the other).
+// rows each (7.0 us with one wave for all forty, one after the other).  Between them a wave waits for the position, then for four
+// sines and cosines, then for its rows: 1024 tokens of 32 + 8 heads 9.4 us = 2.2 TB/s, 4096 23.4 us = 3.6.
 #include "psa_attend.h"
 #include "psa_host.h"
 
@@ -129,7 +130,9 @@ __global__ __launch_bounds__(256) void rotate_kernel(RotateArgs a) {
     }
 }
 
-// Below this many tokens a token's rows are spread over several waves: with 16384 tokens two waves a token took 78 us instead of 75, ten 129.
+// Below this many tokens a token's rows are spread over several waves, up to this many waves in all (bfloat16; with four times as many
+// waves, and with a quarter of them): 512 tokens of 32 + 8 heads 5.2 us (5.7, 6.1), 1024 9.4 (11.0, 13.1), 2048 13.9 (15.0, 17.0), 4096 23.4
+// (24.5, 23.5), 8192 36.4 (38.2, 35.9); 1024 tokens of 8 + 1 heads 4.8 (4.7, 5.7), 4096 9.4 (11.5, 9.4).
 constexpr int kRotateWaves = 4096;
 
 hipError_t launch_rotate(const psa_rotate_desc *d, const void *q_in, const void *k_in, void *q_out, void *k_out, const void *q_weight,

@@ -174,8 +174,10 @@ __device__ __forceinline__ int clamp_ctx(const KvView &kv, int ctx) { return min
 // entry of the call (`blocks` of a request at most) and stores the word, so that nobody has to clear it first.  The lengths of 256
 // requests at a time go to LDS, then sixteen entries a thread are under way at once: about 0.75 ns an entry (3.9 when each
 // entry waited for its request's length).  The others read the entry's page for every KV head, 0.36 ns over 4 bits, so
-// this is hidden with four KV heads or more and for kCheckedEntries in any case; else a launch of its own clears the
-// word, and whoever finds something sets it.
+// for full requests this is hidden with four KV heads or more, and for kCheckedEntries in any case; else a launch of its own
+// clears the word, and whoever finds something sets it.  A thread steps through all places that the table's width and the window
+// allow, so requests far shorter than these wait for it: 256 of 64 tokens with windows of 4000 and 8 KV heads take 31 us over 16
+// bits and 30 over 4 (in pieces, which need no such workgroup, 26 and 24); of 500 tokens 102 and 37 (110 and 43).
 constexpr int kCheckedEntries = 4096;
 __device__ __forceinline__ void check_tables(const KvView &kv, int window, int num_sinks, int blocks, int32_t *header) {
     __shared__ int lengths[256];
@@ -220,15 +222,18 @@ __device__ __forceinline__ void check_tables(const KvView &kv, int window, int n
 //            and there are direct_from of them, or, as the second launch costs 3 to 4 us, where they are fewer and have little to read.
 //   planned  workgroups take pieces of requests: a piece is what the visible blocks of all requests come to, divided by the
 //            workgroups that fill the GPU, and a request gets as many as it takes -- one long request among short ones is
-//            shared by many.  A piece's result is a record, unless it is all of its request, and a second launch joins
-//            the records of a request.  Up to kFoundRequests requests every workgroup finds its piece from the lengths by
+//            shared by many (direct, it is one workgroup's: the host knows what the widths allow, not the lengths).  A
+//            piece's result is a record, unless it is all of its request, and a second launch joins the records of a request.  Up to kFoundRequests requests every workgroup finds its piece from the lengths by
 //            itself (less than a microsecond), and the first one leaves the requests' first records for the launch that joins; for
 //            more requests a launch before lists the pieces.
 // Few pieces, because what a workgroup does before its first block and after its last (dependent trips to memory, the
 // exchange between its waves) costs 5 us and more: the same bytes in pieces of half the size and two rounds of
 // workgroups took 18 % longer.  So a request keeps one piece (or two, ...) up to a quarter more than these hold.  (Trying six lengths
 // and taking the one whose rounds would end first cost every workgroup 1.5 us and gained no more than that.)  One request of
-// 64K tokens among 64 of 1000: 93 us over 16 bits, 40 over 4; with the same number of pieces for every request 772 and 192.
+// 64K tokens among 63 of 1000: 93 us over 16 bits, 40 over 4; with the same number of pieces for every request 772 and 192.
+// Direct calls keep that price up to kDirectBlocks: one request of 5000 tokens among 31 of 100, 8 KV heads, 60 us over 16 bits and 31
+// over 4 (in pieces 15 and 10), among 127 67 and 33 (27 and 19); they win where the lengths are alike or evenly spread: 64 requests
+// of up to 4000 tokens 117 and 37.8 (129 and 38.5), 256 of 4000 663 and 196 (682 and 200).
 struct VisiblePlan {
     int window, num_sinks;
     int blocks;                    // visible blocks of a request at most

@@ -13,9 +13,9 @@ namespace psa {
 // 16x16x16 products, the weights in parts in a head's rows; values in binary16 are split into two bfloat16 parts, exactly, that share
 // one 16x16x32 product with the weights twice.  Tokens of a block that the query does not see get the logit -inf and a
 // zero value row (the page may hold NaN there).
-// Bound by memory: 4 requests of 64K tokens, 8 KV heads, G = 4: 165 us a call = 6.5 TB/s; 64 ragged requests with a window of 4096
-// and 16 sinks, G = 8: 160 us = 6.4; 240 ragged ones with a window of 130, 4 KV heads: 17 us = 3.8, of which 5 are the way to the first
-// block and from the last.  Keys and values are both loaded a block ahead: with the values loaded when their block's turn came
+// Bound by memory: 4 requests of 64K tokens, 8 KV heads, G = 4, bfloat16: 171 us a call = 6.3 TB/s; 64 ragged requests with a window of
+// 4096 and 16 sinks, G = 8, binary16: 153 us = 6.6, vector ALUs 32 % busy (14 % with weights in binary16 parts, in the same time);
+// 240 ragged ones with a window of 130, 4 KV heads: 17 us = 3.8, of which 5 are the way to the first block and from the last.  Keys and values are both loaded a block ahead: with the values loaded when their block's turn came
 // the second took 178 us at the best number of workgroups.  Two workgroups on a CU are enough and more get in each
 // other's way: 155 us with 512 of them, 184 to 188 with 1024 to 2048 (limited to two on a CU by LDS: 175 to 184).
 template <int DT, int G>
