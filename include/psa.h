@@ -301,8 +301,8 @@ psa_status psa_dense_attention(const psa_kv_desc *desc, const void *q, float *ou
  *   window, num_sinks  >= 0, in tokens, of any size: a window of INT32_MAX attends everything, a window of 0 the sinks
  *                      alone, both 0 nothing
  *   out  [batch][num_q_heads][head_dim] float32; lse [batch][num_q_heads] float32 natural-log sum of exponentiated scaled
- *        logits, may be NULL.  Where nothing is visible, or nothing but logits of -inf, out = 0 and lse = -inf; a NaN in a visible key or value shows in the
- *        outputs of its heads, an infinity in a visible value gives infinities or NaN
+ *        logits, may be NULL.  Where nothing is visible, or nothing but logits of -inf, out = 0 and lse = -inf; a NaN in a visible
+ *        key or value shows in the outputs of its heads, an infinity in a visible value gives infinities or NaN
  *   workspace  psa_window_workspace_bytes of the same descriptor, window and num_sinks; holds the sticky error word
  * A call repeated gives the same bits.  How a request is cut, and with it the order of its sums, follows from the batch, the lengths of
  * all its requests, the width of the block table (max_blocks_per_seq), the head counts, window and num_sinks: its results can differ in
